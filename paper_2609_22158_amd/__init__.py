@@ -3,9 +3,10 @@
 The pass lives in libstepkv.so (hand-written HIP kernels behind the C ABI of
 include/stepkv.h); ``binding`` is its ctypes binding. Importing this package
 loads nothing; the first binding call loads the library and raises if it has
-not been built.
+not been built. ``cache4`` is the binding of the 4-bit cache
+(include/stepkv_cache4.h) and of the attention that reads it.
 """
-from . import binding  # noqa: F401
+from . import binding, cache4  # noqa: F401
 from .binding import (  # noqa: F401
     Params,
     Problem,
@@ -30,4 +31,14 @@ from .binding import (  # noqa: F401
     step_utilities,
     text_cues,
     window_lse,
+)
+from .cache4 import (  # noqa: F401
+    Cache4,
+    advance4,
+    append4,
+    compact4,
+    decode_attention4,
+    decode_sparse4,
+    read4,
+    select_blocks4,
 )
