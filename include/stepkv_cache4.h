@@ -144,7 +144,7 @@ size_t stepkv_cache4_decode_workspace_bytes(const stepkv_cache4* c, int32_t num_
  * not above every entry before it, is passed over, and so are the entries past
  * as many as the sequence has blocks.
  * A NaN in an attended key, value or query makes its results NaN. fp32 sums of
- * bf16 products, the probabilities as two bf16 parts (to 2^-16). Results do
+ * exact products, the probabilities in fp32. Results do
  * not depend on other sequences' contents; they are the same from call to call.
  * Errors: EINVAL, EUNSUPPORTED (d), EWORKSPACE (below
  * stepkv_cache4_decode_workspace_bytes, or not 256-byte aligned), EHIP. */

@@ -56,13 +56,14 @@ struct Attend4Args {
   const int32_t* blocks;     // [L][S][H][nlist] or null
   float* out;                // [L][S][Hq][d]
   float* lse;                // [L][S][Hq] or null
-  float* partial;            // [L*H*tiles][splits][16][d+2]: o, m (log2), z
+  float* partial;            // [L*H*tiles][splits][min(G, 16)][d+2]: o, m (log2), z
   int Hq, G, nlist;
   int splits;                // split slots of a (layer, KV head)
   int min_rows;              // least rows of a split
+  int single;                // nonzero: a sequence is one split, written without a merge
   float scale;
 };
-// Fills splits and min_rows from the shape and the rooms of the sequences.
+// Fills splits, min_rows and single from the shape and the rooms of the sequences.
 void plan_attend4(Attend4Args& a, const int32_t* cu_rows_host);
 size_t attend4_partial_floats(const Attend4Args& a);
 hipError_t launch_attend4(const Attend4Args& a, hipStream_t st);

@@ -8,45 +8,63 @@
 // even code and saturation at 6, is the format's).
 #include "cache4_device.h"
 
+#include <type_traits>
+
 namespace stepkv {
 namespace {
 
 constexpr int kThreads = 256;
 
-// max(x, x of lane ^ 1) and ^ 2 (quad permutes): the maximum of four lanes.
-__device__ __forceinline__ uint32_t quad_max(uint32_t x) {
-  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xf, 0xf, true));
-  return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xf, 0xf, true));
+typedef short i16x2_t __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pk_max_u16(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, a),
+                                                                __builtin_bit_cast(u16x2_t, b)));
+}
+__device__ __forceinline__ uint32_t pk_max_i16(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(i16x2_t, a),
+                                                                __builtin_bit_cast(i16x2_t, b)));
+}
+__device__ __forceinline__ uint32_t pk_min_i16(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(i16x2_t, a),
+                                                                __builtin_bit_cast(i16x2_t, b)));
+}
+// Two bf16 patterns as 16-bit integers in the order of their values, and back
+// (its own inverse): negative ones have their magnitude bits inverted.
+__device__ __forceinline__ uint32_t pk_sortable(uint32_t x) {
+  const i16x2_t v = __builtin_bit_cast(i16x2_t, x);
+  return x ^ (__builtin_bit_cast(uint32_t, v >> 15) & 0x7fff7fffu);
 }
 
-// min and max that keep a NaN.
-__device__ __forceinline__ float min_nan(float a, float b) { return a < b || a != a ? a : b; }
-__device__ __forceinline__ float max_nan(float a, float b) { return a > b || a != a ? a : b; }
+// x[i] of an array that stays unchanged for the whole launch, read through the
+// constant address space: with a wave-uniform index the load is a scalar one,
+// which does not queue behind the rows that the compute unit streams.
+__device__ __forceinline__ int read_const(const int32_t* x, int i) {
+  return ((const __attribute__((address_space(4))) int32_t*)x)[i];
+}
 
 // Eight values of a group (the other 24 in the other lanes of the quad):
 // their codes, and the group's scale byte. With the largest magnitude
 // 1.m * 2^E in bf16 bits (E and the 7 bits of m), max <= 7 * 2^e means
 // e = E - 2 for 1.m <= 1.75 (m <= 96) and E - 1 above: a carry into E.
 __device__ __forceinline__ uint32_t quantise8(u32x4_t x, uint32_t& byte) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    top = max(top, max(x[i] & 0x7fffu, (x[i] >> 16) & 0x7fffu));
-  top = quad_max(top);
-  if (top >= 0x7f80u) {  // a NaN or an infinity in the group
-    byte = 255u;
-    return 0u;
-  }
-  byte = (uint32_t)min(max((int)((top + 31u) >> 7) - 2, 3), 252);
-  const float s = scale_of(byte);
-  // (a bit cast of a vector's element takes the vector's first: elements are copied)
   const uint32_t x0 = x[0], x1 = x[1], x2 = x[2], x3 = x[3];
+  uint32_t two = pk_max_u16(pk_max_u16(x0 & 0x7fff7fffu, x1 & 0x7fff7fffu),
+                            pk_max_u16(x2 & 0x7fff7fffu, x3 & 0x7fff7fffu));
+  // over the quad's lanes (^ 1, ^ 2)
+  two = pk_max_u16(two, (uint32_t)__builtin_amdgcn_mov_dpp((int)two, 0xB1, 0xf, 0xf, true));
+  two = pk_max_u16(two, (uint32_t)__builtin_amdgcn_mov_dpp((int)two, 0x4E, 0xf, 0xf, true));
+  const uint32_t top = max(two & 0xffffu, two >> 16);
+  const bool bad = top >= 0x7f80u;  // a NaN or an infinity in the group
+  byte = bad ? 255u : (uint32_t)min(max((int)((top + 31u) >> 7) - 2, 3), 252);
+  const float s = scale_of(byte);
   uint32_t w = 0;
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, x0), s, 0);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, x1), s, 1);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, x2), s, 2);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, x3), s, 3);
-  return w;
+  return bad ? 0u : w;
 }
 
 // The tokens [j0, j1) of sequence s that a call writes (j0 may be negative:
@@ -64,9 +82,28 @@ __device__ __forceinline__ void span_of(const Write4Args& a, int s, int& j0, int
   }
 }
 
+// The span of one sequence, wave-uniform: scalar loads.
+__device__ __forceinline__ void span_const(const Write4Args& a, int s, int& j0, int& j1,
+                                           int& src0, int& src1, int& row0) {
+  row0 = read_const(a.c.cu_rows, s);
+  const int room = read_const(a.c.cu_rows, s + 1) - row0;
+  src0 = read_const(a.cu_src, s);
+  src1 = read_const(a.cu_src, s + 1);
+  if (a.idx) {
+    j0 = 0;
+    j1 = min(min(read_const(a.cu_retained, s + 1) - read_const(a.cu_retained, s), src1 - src0),
+             room);
+  } else {
+    const int len = max(read_const(a.c.lens, s), 0);
+    j0 = len - max(src1 - src0, 0);
+    j1 = min(len, room);
+  }
+}
+
 // One workgroup per (layer, KV head, block of 64 tokens): a lane holds 16
 // bytes (8 channels) of a row, a quad of lanes a group. The block's bounds of
-// K are taken from the values as quantised.
+// K are taken from the values as quantised, as ordered 16-bit integers; a NaN
+// is a flag beside them.
 template <int D>
 __global__ __launch_bounds__(kThreads) void write4_kernel(Write4Args a) {
   constexpr int PR = D / 8;             // pieces of 8 channels a row
@@ -74,7 +111,8 @@ __global__ __launch_bounds__(kThreads) void write4_kernel(Write4Args a) {
   constexpr int NP = kBlock4 / RP;      // passes
   constexpr int NS = D / kGroup4;
   constexpr int NWV = kThreads / kWave;
-  __shared__ float red[NWV][2][D];
+  __shared__ uint32_t red[NWV][2][D / 2];
+  __shared__ int bad_s[NWV][PR];
   const int tid = threadIdx.x;
   const Cache4View& c = a.c;
   if (blockIdx.x == 0 && tid == 0) {
@@ -91,20 +129,20 @@ __global__ __launch_bounds__(kThreads) void write4_kernel(Write4Args a) {
     }
   }
   if (a.nblocks == 0) return;
-  const int lh = blockIdx.x / a.nblocks;
-  const int l = lh / c.H, h = lh - l * c.H;
-  int s, first;
-  locate_item(c.S, (int)(blockIdx.x - lh * a.nblocks), [&](int sq) {
-    int j0, j1, src0;
-    span_of(a, sq, j0, j1, src0);
-    j0 = max(j0, 0);
-    return j1 > j0 ? (j1 - 1) / kBlock4 - j0 / kBlock4 + 1 : 0;
-  }, s, first);
+  const int lh = uniform(blockIdx.x / a.nblocks), at = uniform(blockIdx.x - lh * a.nblocks);
+  const int l = uniform(lh / c.H), h = lh - l * c.H;
+  int s = 0, first = 0, j0, j1, src0, src1, row0;
+  if (c.S > 1)
+    locate_item(c.S, at, [&](int sq) {
+      int b0, b1, unused;
+      span_of(a, sq, b0, b1, unused);
+      b0 = max(b0, 0);
+      return b1 > b0 ? (b1 - 1) / kBlock4 - b0 / kBlock4 + 1 : 0;
+    }, s, first);
   if (s < 0) return;  // past the last block: uniform over the workgroup
-  int j0, j1, src0;
-  span_of(a, s, j0, j1, src0);
-  const int blk = max(j0, 0) / kBlock4 + ((int)(blockIdx.x - lh * a.nblocks) - first);
-  const int seq_rows = a.idx ? a.cu_src[s + 1] - src0 : 0;
+  span_const(a, s, j0, j1, src0, src1, row0);
+  const int blk = max(j0, 0) / kBlock4 + (at - first);
+  if (blk * kBlock4 >= j1) return;  // past the only sequence's last block
   const int32_t* __restrict__ idx =
       a.idx ? a.idx + (a.shared_idx ? 0 : (size_t)lh * a.nsrc) + src0 : nullptr;
   const int sub = tid / PR, piece = tid % PR;
@@ -116,7 +154,7 @@ __global__ __launch_bounds__(kThreads) void write4_kernel(Write4Args a) {
     if (j >= j0 && j < j1) {
       if (idx) {
         const int pos = idx[j];
-        if (pos >= 0 && pos < seq_rows) src[p] = src0 + pos;
+        if (pos >= 0 && pos < src1 - src0) src[p] = src0 + pos;
       } else if (src0 + (j - j0) >= 0 && src0 + (j - j0) < a.nsrc) {
         src[p] = src0 + (j - j0);
       }
@@ -132,36 +170,37 @@ __global__ __launch_bounds__(kThreads) void write4_kernel(Write4Args a) {
     kx[p] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(kb + src[p] * a.k_row));
     vx[p] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(vb + src[p] * a.v_row));
   }
-  const size_t row0 = (size_t)lh * c.rows + c.cu_rows[s] + (size_t)blk * kBlock4;
-  float lo[8], hi[8];
+  const size_t first_row = (size_t)lh * c.rows + row0 + (size_t)blk * kBlock4;
+  uint32_t lo[4], hi[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    lo[i] = INFINITY;
-    hi[i] = -INFINITY;
+  for (int i = 0; i < 4; ++i) {
+    lo[i] = 0x7f807f80u;  // +inf, and -inf as it sorts
+    hi[i] = pk_sortable(0xff80ff80u);
   }
   uint32_t flags = 0;
+  bool bad = false;  // a NaN among this lane's channels of K
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
     uint32_t kbyte, vbyte;  // every lane: the quad exchanges need all four
     const uint32_t kw = quantise8(kx[p], kbyte), vw = quantise8(vx[p], vbyte);
     if (src[p] < 0) continue;
     if (kbyte == 255u || vbyte == 255u) flags |= kFlagNonFinite4;
-    const size_t row = row0 + p * RP + sub;
-    reinterpret_cast<uint32_t*>(c.k_codes + row * (D / 2))[piece] = kw;
-    reinterpret_cast<uint32_t*>(c.v_codes + row * (D / 2))[piece] = vw;
+    const size_t row = first_row + p * RP + sub;
+    __builtin_nontemporal_store(kw, reinterpret_cast<uint32_t*>(c.k_codes + row * (D / 2)) + piece);
+    __builtin_nontemporal_store(vw, reinterpret_cast<uint32_t*>(c.v_codes + row * (D / 2)) + piece);
     if (piece % 4 == 0) {
       c.k_scales[row * NS + piece / 4] = (uint8_t)kbyte;
       c.v_scales[row * NS + piece / 4] = (uint8_t)vbyte;
     }
-    if (c.k_bounds) {
+    if (kbyte == 255u) {
+      bad = true;
+    } else {
       const u32x4_t y = spread8(kw, scale_of(kbyte));
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float y0 = bf16_float(y[i] & 0xffffu), y1 = bf16_float(y[i] >> 16);
-        lo[2 * i] = min_nan(lo[2 * i], y0);
-        hi[2 * i] = max_nan(hi[2 * i], y0);
-        lo[2 * i + 1] = min_nan(lo[2 * i + 1], y1);
-        hi[2 * i + 1] = max_nan(hi[2 * i + 1], y1);
+        const uint32_t t = pk_sortable(y[i]);
+        lo[i] = pk_min_i16(lo[i], t);
+        hi[i] = pk_max_i16(hi[i], t);
       }
     }
   }
@@ -169,36 +208,49 @@ __global__ __launch_bounds__(kThreads) void write4_kernel(Write4Args a) {
   if (!c.k_bounds) return;
   // over the rows of the wave (lanes of one piece), then over the waves
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int off = PR; off < kWave; off <<= 1) {
 #pragma unroll
-    for (int off = PR; off < kWave; off <<= 1) {
-      lo[i] = min_nan(lo[i], __shfl_xor(lo[i], off, kWave));
-      hi[i] = max_nan(hi[i], __shfl_xor(hi[i], off, kWave));
+    for (int i = 0; i < 4; ++i) {
+      lo[i] = pk_min_i16(lo[i], (uint32_t)__shfl_xor((int)lo[i], off, kWave));
+      hi[i] = pk_max_i16(hi[i], (uint32_t)__shfl_xor((int)hi[i], off, kWave));
     }
+  }
+  const uint64_t bads = ballot(bad);
   if ((tid & 63) < PR) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      red[tid >> 6][0][8 * piece + i] = lo[i];
-      red[tid >> 6][1][8 * piece + i] = hi[i];
+    for (int i = 0; i < 4; ++i) {
+      red[tid >> 6][0][4 * piece + i] = lo[i];
+      red[tid >> 6][1][4 * piece + i] = hi[i];
     }
+    uint64_t lanes = 0;  // those that hold this piece
+#pragma unroll
+    for (int off = 0; off < kWave; off += PR) lanes |= uint64_t(1) << off;
+    bad_s[tid >> 6][piece] = (bads & (lanes << piece)) != 0;
   }
   __syncthreads();
   uint16_t* __restrict__ bounds =
-      c.k_bounds + ((size_t)lh * c.nblk + c.cu_rows[s] / kBlock4 + s + blk) * 2 * D;
-  const bool opened = blk * kBlock4 >= j0;  // the block's first token is among the new ones
+      c.k_bounds + ((size_t)lh * c.nblk + row0 / kBlock4 + s + blk) * 2 * D;
   if (tid < D) {
-    const int which = tid / (D / 2), ch = 2 * (tid % (D / 2));
-    float x0 = red[0][which][ch], x1 = red[0][which][ch + 1];
-    auto join = [&](float y0, float y1) {
-      x0 = which ? max_nan(x0, y0) : min_nan(x0, y0);
-      x1 = which ? max_nan(x1, y1) : min_nan(x1, y1);
-    };
+    const int which = tid / (D / 2), two = tid % (D / 2);  // channels 2 two, 2 two + 1
+    uint32_t x = red[0][which][two];
+    bool nan0 = false, nan1;
 #pragma unroll
-    for (int w = 1; w < NWV; ++w) join(red[w][which][ch], red[w][which][ch + 1]);
-    uint32_t* at = reinterpret_cast<uint32_t*>(bounds + which * D + ch);
-    if (!opened) join(bf16_float(*at & 0xffffu), bf16_float(*at >> 16));
-    // exact: the values are bf16
-    *at = (__float_as_uint(x0) >> 16) | (__float_as_uint(x1) & 0xffff0000u);
+    for (int w = 0; w < NWV; ++w) {
+      x = which ? pk_max_i16(x, red[w][which][two]) : pk_min_i16(x, red[w][which][two]);
+      nan0 |= bad_s[w][two / 4] != 0;
+    }
+    nan1 = nan0;
+    uint32_t* out = reinterpret_cast<uint32_t*>(bounds + which * D) + two;
+    if (blk * kBlock4 < j0) {  // the block's first token is not among the new ones
+      const uint32_t old = *out, t = pk_sortable(old);
+      nan0 |= (old & 0x7fffu) > 0x7f80u;
+      nan1 |= (old >> 16 & 0x7fffu) > 0x7f80u;
+      x = which ? pk_max_i16(x, t) : pk_min_i16(x, t);
+    }
+    x = pk_sortable(x);
+    if (nan0) x = (x & 0xffff0000u) | 0x7fc0u;
+    if (nan1) x = (x & 0xffffu) | 0x7fc00000u;
+    *out = x;
   }
 }
 
@@ -208,49 +260,79 @@ __global__ void advance4_kernel(Cache4View c, const int32_t* __restrict__ cu_new
 }
 
 // A thread per 8 channels of a row: one word of codes and a scale byte in, 16
-// bytes out, several rows in flight per thread.
-constexpr int kReadPasses = 2;
+// bytes out, PASSES rows in flight per thread. A workgroup's rows almost always
+// belong to one sequence, whose bounds are then found once, with scalar loads.
 
-template <int D>
+template <int D, int PASSES>
 __global__ __launch_bounds__(kThreads) void read4_kernel(Read4Args a) {
   constexpr int PR = D / 8;
   constexpr int RP = kThreads / PR;
-  constexpr int RB = RP * kReadPasses;
+  constexpr int RB = RP * PASSES;
   constexpr int NS = D / kGroup4;
   const Cache4View& c = a.c;
   const int nb = (a.out_rows + RB - 1) / RB;
-  const int lh = blockIdx.x / nb, rb = blockIdx.x - lh * nb;
-  const int total = min(a.out_rows, a.cu_out[c.S]);
+  const int bid = blockIdx.x;
+  const int lh = uniform(bid / nb), o0 = (bid - lh * nb) * RB;
+  if (lh >= c.L * c.H) return;
+  const int total = min(a.out_rows, read_const(a.cu_out, c.S));
+  if (o0 >= total) return;
   const int sub = threadIdx.x / PR, piece = threadIdx.x % PR;
-  int64_t row[kReadPasses];  // cache row, or -1
+  // row i of sequence s's rows is token len - n + i, in cache row shift + o
+  int lo = 0, hi = c.S;  // cu_out[lo] <= o0 < cu_out[hi] where cu_out is in order
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (read_const(a.cu_out, mid) <= o0) lo = mid;
+    else hi = mid;
+  }
+  auto span = [&](int s, int& b, int& e, int64_t& shift) {  // rows [b, e) have tokens
+    const int r0 = read_const(a.cu_out, s), r1 = read_const(a.cu_out, s + 1);
+    const int row0 = read_const(c.cu_rows, s);
+    const int len = max(read_const(c.lens, s), 0);
+    const int held = min(len, read_const(c.cu_rows, s + 1) - row0);
+    // token of row o: o - r1 + len, within [0, held)
+    b = (int)max((int64_t)r0, (int64_t)r1 - len);
+    e = (int)min((int64_t)r1, (int64_t)r1 - len + held);
+    shift = (int64_t)row0 + len - r1;
+  };
+  int b, e;
+  int64_t shift;
+  span(lo, b, e, shift);
+  const bool one = o0 + RB <= read_const(a.cu_out, lo + 1) || lo + 1 == c.S;
+  int64_t row[PASSES];  // cache row, or -1
 #pragma unroll
-  for (int p = 0; p < kReadPasses; ++p) {
-    const int o = rb * RB + p * RP + sub;
+  for (int p = 0; p < PASSES; ++p) {
+    const int o = o0 + p * RP + sub;
     row[p] = -1;
     if (o >= total) continue;
-    const int s = segment_of(a.cu_out, c.S, o);
-    const int i = o - a.cu_out[s], n = a.cu_out[s + 1] - a.cu_out[s];
-    const int j = max(c.lens[s], 0) - n + i;
-    if (i >= 0 && i < n && j >= 0 && j < held_tokens(c, s))
-      row[p] = (int64_t)lh * c.rows + c.cu_rows[s] + j;
+    if (!one && o >= read_const(a.cu_out, lo + 1)) {
+      const int s = segment_of(a.cu_out, c.S, o);
+      const int r1 = a.cu_out[s + 1], len = max(c.lens[s], 0);
+      const int64_t j = (int64_t)o - r1 + len;
+      if (o >= a.cu_out[s] && o < r1 && j >= 0 && j < held_tokens(c, s))
+        row[p] = (int64_t)lh * c.rows + c.cu_rows[s] + j;
+    } else if (o >= b && o < e) {
+      row[p] = (int64_t)lh * c.rows + shift + o;
+    }
   }
-  uint32_t kw[kReadPasses], vw[kReadPasses], ks[kReadPasses], vs[kReadPasses];
+  uint32_t kw[PASSES], vw[PASSES], ks[PASSES], vs[PASSES];
 #pragma unroll
-  for (int p = 0; p < kReadPasses; ++p) {
+  for (int p = 0; p < PASSES; ++p) {
     if (row[p] < 0) continue;
     if (a.k_out) {
-      kw[p] = reinterpret_cast<const uint32_t*>(c.k_codes + row[p] * (D / 2))[piece];
+      kw[p] = __builtin_nontemporal_load(
+          reinterpret_cast<const uint32_t*>(c.k_codes + row[p] * (D / 2)) + piece);
       ks[p] = c.k_scales[row[p] * NS + piece / 4];
     }
     if (a.v_out) {
-      vw[p] = reinterpret_cast<const uint32_t*>(c.v_codes + row[p] * (D / 2))[piece];
+      vw[p] = __builtin_nontemporal_load(
+          reinterpret_cast<const uint32_t*>(c.v_codes + row[p] * (D / 2)) + piece);
       vs[p] = c.v_scales[row[p] * NS + piece / 4];
     }
   }
 #pragma unroll
-  for (int p = 0; p < kReadPasses; ++p) {
+  for (int p = 0; p < PASSES; ++p) {
     if (row[p] < 0) continue;
-    const size_t dst = ((size_t)lh * a.out_rows + rb * RB + p * RP + sub) * D;
+    const size_t dst = ((size_t)lh * a.out_rows + o0 + p * RP + sub) * D;
     if (a.k_out)
       __builtin_nontemporal_store(spread8(kw[p], scale_of(ks[p])),
                                   reinterpret_cast<u32x4_t*>(a.k_out + dst) + piece);
@@ -278,12 +360,23 @@ hipError_t launch_advance4(const Cache4View& c, const int32_t* cu_new, hipStream
 }
 
 hipError_t launch_read4(const Read4Args& a, hipStream_t st) {
-  const int rb = kThreads / (a.c.d / 8) * kReadPasses;
-  const dim3 grid((unsigned)(a.c.L * a.c.H) * (unsigned)((a.out_rows + rb - 1) / rb));
-  if (a.c.d == 128)
-    hipLaunchKernelGGL(read4_kernel<128>, grid, dim3(kThreads), 0, st, a);
-  else
-    hipLaunchKernelGGL(read4_kernel<64>, grid, dim3(kThreads), 0, st, a);
+  // One row per thread keeps the most workgroups in flight, and the smallest
+  // calls short (32 layers x 8 heads x 1536 rows 42 us, with four rows 47; 85
+  // rows 4.1 and 6.0). With many rows of several sequences the search for the
+  // sequence counts: four rows share it (28 layers x 4 heads x 16 sequences,
+  // 28800 rows in all: 358 us, with one row 380).
+  const int rp = kThreads / (a.c.d / 8);
+  const int64_t one = (int64_t)a.c.L * a.c.H * ((a.out_rows + rp - 1) / rp);
+  auto run = [&](auto passes) {
+    constexpr int P = decltype(passes)::value;
+    const dim3 grid((unsigned)(a.c.L * a.c.H) * (unsigned)((a.out_rows + P * rp - 1) / (P * rp)));
+    if (a.c.d == 128)
+      hipLaunchKernelGGL((read4_kernel<128, P>), grid, dim3(kThreads), 0, st, a);
+    else
+      hipLaunchKernelGGL((read4_kernel<64, P>), grid, dim3(kThreads), 0, st, a);
+  };
+  if (a.c.S > 1 && one >= 8 * 2048) run(std::integral_constant<int, 4>{});
+  else run(std::integral_constant<int, 1>{});
   return hipGetLastError();
 }
 

@@ -28,27 +28,36 @@ __device__ __forceinline__ void report_rooms(const Cache4View& c) {
   if (over) atomicOr(c.status, kFlagOutRows4);
 }
 
+// Inclusive prefix sum over the wave's lanes on the vector unit (DPP row shifts
+// within 16 lanes, then the row totals); the wave's total is lane 63's.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);  // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);  // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);  // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31
+  return x;
+}
+__device__ __forceinline__ int wave_total(int scanned) {
+  return __builtin_amdgcn_readlane(scanned, kWave - 1);
+}
+
 // The item `at` of a list that holds count(s) items of each sequence in order:
-// its sequence, and the first item of that sequence. A wave-wide prefix sum
-// over 64 sequences at a time; s_out = -1 past the list's end (grids are sized
-// by bounds that the host knows). Wave-uniform.
+// its sequence, and the first item of that sequence; s_out = -1 past the
+// list's end (grids are sized by bounds that the host knows). Wave-uniform.
 template <typename F>
 __device__ __forceinline__ void locate_item(int S, int at, F count, int& s_out, int& first_out) {
   const int lane = threadIdx.x & 63;
   int base = 0;
   for (int s0 = 0; s0 < S; s0 += kWave) {
     const int cnt = s0 + lane < S ? count(s0 + lane) : 0;
-    int incl = cnt;
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-      const int o = __shfl_up(incl, off, kWave);
-      if (lane >= off) incl += o;
-    }
-    const int total = __shfl(incl, kWave - 1, kWave);
+    const int incl = wave_scan(cnt);
+    const int total = wave_total(incl);
     if (at < base + total) {
       const int k = __builtin_ctzll(ballot(base + incl > at));
-      s_out = uniform(s0 + k);
-      first_out = uniform(base + __shfl(incl - cnt, k, kWave));
+      s_out = s0 + k;
+      first_out = base + __builtin_amdgcn_readlane(incl - cnt, k);
       return;
     }
     base += total;

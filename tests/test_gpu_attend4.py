@@ -3,11 +3,12 @@ of blocks, and the selection of those lists.
 
 Tolerance, per output channel, derived from what is rounded (u = 2^-24, a half step of fp32):
 logits are fp32 sums of exact products of bf16 pairs, off by at most eps = (d + 2) u * scale *
-sum |q k|, and scaled to the log2 domain (2 u |z|, within the same sum); a probability is off by
-a factor of 1 +- (eps + 2^-21 (the exponential, its argument's subtraction among it) + 2^-16 (two
-bf16 parts, half a step 2^-8 each)); sums over n tokens by n u, and as much again for the merges.
-Numerator and denominator both carry it, so |error| <= 2 (eps + 2^-16 + 2^-21 + (2 n + 64) u)
-* sum p |v|. The log-sum-exp: eps + 2^-21 + (2 n + 64) u + 4 u |lse|."""
+sum |q k|, and scaled to the log2 domain (2 u |z|, within the same sum); a probability
+2^x, with x rounded to u |x|, is off by a factor of 1 +- (eps + 2^-19) while |x| <= 40, and below
+2^-40 has no part in what follows; it is multiplied without a rounding (three bf16 parts); sums
+over n tokens are off by n u, and as much again for the merges. Numerator and denominator both
+carry it, so |error| <= 2 (eps + 2^-19 + (2 n + 64) u) * sum p |v|. The log-sum-exp: eps + 2^-19 +
+(2 n + 64) u + 4 u |lse|."""
 import math
 import zlib
 
@@ -75,8 +76,8 @@ class Made:
                     for g, q in enumerate(self.query(l, s, h)):
                         ref, z, spread, reach = R.attend(q, k, v, scale)
                         eps = (self.d + 2) * U * reach
-                        steps = 2.0 ** -21 + (2 * len(k) + 64) * U
-                        tol = 2 * (eps + 2.0 ** -16 + steps) * spread
+                        steps = 2.0 ** -19 + (2 * len(k) + 64) * U
+                        tol = 2 * (eps + steps) * spread
                         got = out[l, s, h * self.G + g]
                         assert (np.abs(got - ref) <= tol).all(), (l, s, h, g, np.abs(got - ref).max(), tol.max())
                         gz = lse[l, s, h * self.G + g]
@@ -398,7 +399,7 @@ def test_the_cycle_of_a_trajectory(gpu_lib):
     gen.manual_seed(2)
     q = torch.randn((L, S, Hq, d), generator=gen, device="cuda").bfloat16()
     one = torch.arange(S + 1, dtype=torch.int32, device="cuda")
-    # the bf16 decode over the rows as read back agrees (both carry P to 2^-16 twice, fp32 sums)
+    # the bf16 decode over the rows as read back agrees (it carries P to 2^-16, twice; fp32 sums)
     k4, v4 = C4.read4(cache, cu_ret, int(cu_ret[-1]))
     ref = B.decode_attention(g.pb, q, k4, v4, cu_ret, int(cu_ret[-1]))
     out = C4.decode_attention4(cache, q)

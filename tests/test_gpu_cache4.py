@@ -310,3 +310,29 @@ def test_layers_without_bounds(gpu_lib):
     k, v = C4.read4(parts.layers(1, 2), cu, 7)
     kw, vw = C4.read4(whole, cu, 7)
     assert torch.equal(k, kw[1:]) and torch.equal(v, vw[1:])
+
+
+def test_read_back_of_many_rows(gpu_lib):
+    """A read of many rows of several sequences (four rows a thread) gives what reads of its layers
+    one by one (one row a thread) do, across the sequences' boundaries."""
+    import torch
+
+    L, H, d, lens = 16, 16, 128, [700, 1, 0, 333, 63]
+    cu_rows = np.concatenate([[0], np.cumsum([n + 5 for n in lens])]).astype(np.int32)
+    cache = C4.Cache4(L, H, d, cu_rows)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(4)
+    cu = torch.tensor([0] + list(np.cumsum(lens)), dtype=torch.int32, device="cuda")
+    C4.advance4(cache, cu)
+    k, v = (torch.randn((L, sum(lens), H, d), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    C4.append4(cache, k, v, cu)
+    for counts in (lens, [600, 0, 5, 333, 62]):  # the second: more than the third sequence has
+        co = torch.tensor([0] + list(np.cumsum(counts)), dtype=torch.int32, device="cuda")
+        n = sum(counts)
+        whole = [torch.full((L, H, n + 70, d), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        C4.read4(cache, co, n + 70, k_out=whole[0], v_out=whole[1])
+        for l in range(L):
+            one = [torch.full((1, H, n + 70, d), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+            C4.read4(cache.layers(l), co, n + 70, k_out=one[0], v_out=one[1])
+            assert torch.equal(one[0][0], whole[0][l]) and torch.equal(one[1][0], whole[1][l])
+    assert (whole[0][:, :, 600:605] == 7).all()
