@@ -69,6 +69,7 @@ _SIGNATURES = {
 }
 
 _lib: Optional[ctypes.CDLL] = None
+_fns: dict = {}  # the library's functions by name
 
 
 def load() -> ctypes.CDLL:
@@ -80,6 +81,8 @@ def load() -> ctypes.CDLL:
             fn = getattr(lib, name)
             fn.restype = res
             fn.argtypes = args
+            _fns[name] = fn
+        _fns["stepkv_status_read"] = lib.stepkv_status_read
         _lib = lib
     return _lib
 
@@ -126,6 +129,7 @@ class Cache4:
         self.k_bounds = k_bounds
         self.lens = buffer(lens, torch.int32, (S,), "lens")
         self.status_dev = torch.zeros(1, dtype=torch.int32, device=dev) if status else None
+        load()
         self._bind()
 
     def _bind(self):
@@ -137,6 +141,8 @@ class Cache4:
                          ptr(self.lens), ptr(self.k_codes), ptr(self.v_codes), ptr(self.k_scales),
                          ptr(self.v_scales), ptr(self.k_bounds), ptr(self.status_dev))
         self._ref = ctypes.byref(self.c)
+        self._sizes = {}    # workspace bytes of a call, by its shape
+        self._strides = {}  # checked strides of new tokens, by their layout
 
     def layers(self, first: int, n: int = 1) -> "Cache4":
         """Layers first .. first + n - 1 as a cache of their own (views; lens is shared)."""
@@ -170,30 +176,31 @@ def _device(device):
 
 
 def _need(t, dtype, shape, name, device):
+    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype != dtype:
         raise TypeError(f"{name}: dtype {t.dtype}, expected {dtype}")
     if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if not t.is_contiguous() or t.device != device:
-        raise ValueError(f"{name}: must be a contiguous tensor on {device}")
-    return t.data_ptr()
+    raise ValueError(f"{name}: must be a contiguous tensor on {device}")
 
 
 def _call(cache, name, stream, *args):
     """The library's `name` on the cache's device; the stream is the last argument."""
     import torch
 
-    fn = getattr(load(), name)
-    if cache.device.type != "cuda":
-        raise ValueError(f"{name}: the cache lies on {cache.device}, not on a GPU")
-    if stream is not None and stream.device != cache.device:
-        raise ValueError(f"{name}: a stream of {stream.device}, the cache lies on {cache.device}")
-    if torch.cuda.current_device() == cache.device.index:
-        rc = fn(*args, B._stream(stream))
+    dev = cache.device
+    if dev.type != "cuda":
+        raise ValueError(f"{name}: the cache lies on {dev}, not on a GPU")
+    if stream is not None and stream.device != dev:
+        raise ValueError(f"{name}: a stream of {stream.device}, the cache lies on {dev}")
+    if torch.cuda.current_device() == dev.index:
+        rc = _fns[name](*args, B._stream(stream))
     else:
-        with torch.cuda.device(cache.device):
-            rc = fn(*args, B._stream(stream))
-    B._check(name, rc)
+        with torch.cuda.device(dev):
+            rc = _fns[name](*args, B._stream(stream))
+    if rc != B.OK:
+        raise B.StepKVError(name, rc)
 
 
 def _empty(shape, dtype, cache, stream):
@@ -206,12 +213,19 @@ def _empty(shape, dtype, cache, stream):
         return torch.empty(shape, dtype=dtype, device=cache.device)
 
 
-def _workspace(workspace, nbytes, cache, stream):
+def _workspace(workspace, cache, stream, size, *args):
+    """The caller's workspace, or one of `size`(cache, *args) bytes: that depends on the shape alone,
+    which a cache keeps."""
     import torch
 
     if workspace is None:
-        workspace = _empty((max(int(nbytes), 1),), torch.uint8, cache, stream)
-    elif workspace.device != cache.device or not workspace.is_contiguous():
+        key = (size, args)
+        nbytes = cache._sizes.get(key)
+        if nbytes is None:
+            nbytes = cache._sizes[key] = max(int(_fns[size](cache._ref, *args)), 1)
+        workspace = _empty((nbytes,), torch.uint8, cache, stream)
+        return workspace, workspace.data_ptr(), nbytes
+    if workspace.device != cache.device or not workspace.is_contiguous():
         raise ValueError(f"workspace: must be a contiguous tensor on {cache.device}")
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
@@ -249,6 +263,10 @@ def _tokens(t, cache, name):
 
     if t.dtype != torch.bfloat16:
         raise TypeError(f"{name}: dtype {t.dtype}, expected {torch.bfloat16}")
+    key = (t.shape, t.stride())
+    strides = cache._strides.get(key)
+    if strides is not None and t.device == cache.device and t.data_ptr() % 16 == 0:
+        return t.data_ptr(), strides
     L, H, d = cache.num_layers, cache.num_kv_heads, cache.head_dim
     if t.dim() != 4 or t.shape[0] != L or t.shape[2] != H or t.shape[3] != d:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected ({L}, tokens, {H}, {d})")
@@ -257,7 +275,11 @@ def _tokens(t, cache, name):
     strides = _i64x3(*(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)))
     if t.numel() and (t.data_ptr() % 16 or any(x % 8 for x in strides)):
         raise ValueError(f"{name}: rows must be 16-byte aligned (strides {t.stride()})")
-    return t.data_ptr() if t.numel() else None, strides
+    if not t.numel():
+        return None, strides
+    if len(cache._strides) < 64:
+        cache._strides[key] = strides
+    return t.data_ptr(), strides
 
 
 def append4(cache: Cache4, k_new, v_new, cu_new, *, stream=None) -> Cache4:
@@ -338,9 +360,7 @@ def decode_attention4(cache: Cache4, q_dec, *, blocks=None, scale: float = 0.0, 
         bp = _need(blocks, torch.int32, (cache.num_layers, cache.num_seqs, cache.num_kv_heads, n),
                    "blocks", cache.device)
     out, op, lse, lp = _results(cache, Hq, out, lse, want_lse, stream)
-    need = (load().stepkv_cache4_decode_workspace_bytes(cache._ref, Hq, n) if workspace is None
-            else 0)
-    ws, wp, wn = _workspace(workspace, need, cache, stream)
+    ws, wp, wn = _workspace(workspace, cache, stream, "stepkv_cache4_decode_workspace_bytes", Hq, n)
     _call(cache, "stepkv_cache4_decode", stream, cache._ref, Hq, qp, bp, n, float(scale), op, lp,
           wp, wn)
     return out if lse is None else (out, lse)
@@ -363,8 +383,7 @@ def select_blocks4(cache: Cache4, q_dec, num_blocks: int, *, first: int = 1, las
     the first and last blocks of every sequence and the best others for the step's queries."""
     qp, Hq = _queries(cache, q_dec)
     blocks, bp = _blocks(cache, num_blocks, blocks, stream)
-    need = load().stepkv_cache4_select_workspace_bytes(cache._ref) if workspace is None else 0
-    ws, wp, wn = _workspace(workspace, need, cache, stream)
+    ws, wp, wn = _workspace(workspace, cache, stream, "stepkv_cache4_select_workspace_bytes")
     _call(cache, "stepkv_cache4_select_blocks", stream, cache._ref, Hq, qp, int(num_blocks),
           int(first), int(last), bp, wp, wn)
     return blocks
@@ -378,9 +397,8 @@ def decode_sparse4(cache: Cache4, q_dec, num_blocks: int, *, first: int = 1, las
     qp, Hq = _queries(cache, q_dec)
     blocks, bp = _blocks(cache, num_blocks, blocks, stream)
     out, op, lse, lp = _results(cache, Hq, out, lse, want_lse, stream)
-    need = (load().stepkv_cache4_sparse_workspace_bytes(cache._ref, Hq, int(num_blocks))
-            if workspace is None else 0)
-    ws, wp, wn = _workspace(workspace, need, cache, stream)
+    ws, wp, wn = _workspace(workspace, cache, stream, "stepkv_cache4_sparse_workspace_bytes", Hq,
+                            int(num_blocks))
     _call(cache, "stepkv_cache4_decode_sparse", stream, cache._ref, Hq, qp, int(num_blocks),
           int(first), int(last), float(scale), bp, op, lp, wp, wn)
     return (out, blocks) if lse is None else (out, blocks, lse)

@@ -512,11 +512,12 @@ __global__ __launch_bounds__(THREADS) void combine4_kernel(Attend4Args a) {
 
 }  // namespace
 
-// Splits for the rooms. Sequences of at most 512 rows are one split each, which
-// needs no merge (4 heads x 300 rows, d 64: 5.0 us, with splits of 128 rows and
-// the merge 7.9), and so are those of at most 1024 rows where they fill the chip
-// (28 layers x 4 heads x 16 sequences x 1024 rows, G 7: 57 us, in 26 splits a
-// (layer, head) and the merge 94). Otherwise about 4096 rows a split (a wave's
+// Splits for the rooms. Short sequences are one split each, which needs no merge;
+// 8 waves share it while there are at most 256. Such a step takes about 5.5 us and
+// 4.2 ns a row of the longest sequence (d 64: 2.5 ns), splits and their merge 8.5
+// us and more for more sequences (8 heads, d 128, one sequence of 600 rows: 7.6 us
+// in one split, 8.6 in many; of 1536 11.3, 8.5; 16 sequences of 600: 8.5, 13.1; of
+// 2048 14.9, 19.0; 28 layers x 4 heads x 16 sequences x 1024: 57, 94). Otherwise about 4096 rows a split (a wave's
 // start and merge cost about three tiles; 8 layers x 8 heads x 131071 rows: 1024
 // rows 226 us, 2048 197, 4096 193, 8192 197), but enough splits for four
 // workgroups on each of the 256 compute units while those have a tile per wave.
@@ -531,7 +532,9 @@ void plan_attend4(Attend4Args& a, const int32_t* cu_rows_host) {
     longest = std::max(longest, n);
     most += (n + a.min_rows - 1) / a.min_rows;
   }
-  a.single = longest <= 512 || (longest <= 1024 && units * a.c.S >= 1024);
+  const int64_t rows = units * a.c.S;  // workgroups of one split a sequence
+  const int64_t most_single = rows > 256 ? 1024 : std::min<int64_t>(2048, 640 + 12 * rows);
+  a.single = longest * (a.c.d + 64) / 192 <= most_single;
   if (a.single) {
     a.splits = a.c.S;
     return;

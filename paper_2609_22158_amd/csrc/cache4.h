@@ -75,10 +75,11 @@ struct Select4Args {
   uint64_t* keys;            // workspace [L*H][nblk]: ordered scores
   int32_t* blocks;           // [L][S][H][n]
   int Hq, G, n, first, last;
-  int chunks;                // score chunks of a (layer, KV head)
+  int chunks;                // score chunks of a (layer, KV head); 0: scored where selected
+  int most;                  // blocks that the longest sequence has room for
 };
-// Chunks of the score kernel for these rooms.
-int score4_chunks(const int32_t* cu_rows_host, int S);
+// Fills chunks and most from the shape and the rooms of the sequences.
+void plan_select4(Select4Args& a, const int32_t* cu_rows_host);
 hipError_t launch_select4(const Select4Args& a, hipStream_t st);
 
 }  // namespace stepkv

@@ -139,7 +139,7 @@ int run_select(const stepkv_cache4* c, int32_t num_q_heads, const void* q_dec,
   a.n = num_blocks;
   a.first = first_blocks;
   a.last = last_blocks;
-  a.chunks = score4_chunks(c->cu_rows_host, c->num_seqs);
+  plan_select4(a, c->cu_rows_host);
   if (!grid_fits((int64_t)c->num_layers * c->num_kv_heads * a.chunks)) return STEPKV_EUNSUPPORTED;
   return hip_status(launch_select4(a, st));
 }
