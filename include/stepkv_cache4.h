@@ -57,6 +57,9 @@ extern "C" {
 
 #define STEPKV_CACHE4_BLOCK 64 /* tokens of a block */
 #define STEPKV_CACHE4_GROUP 32 /* channels of a scale */
+/* Rows of a (layer, KV head), cu_rows[S] (EUNSUPPORTED beyond): sums of rows and
+ * of a split's length stay within 31 bits. */
+#define STEPKV_CACHE4_MAX_ROWS ((1 << 30) - (1 << 20))
 
 /* A cache: its shape, the rows of its sequences, and its device buffers (all
  * owned by the caller). The layers l0 .. l0 + n - 1 of a cache are a cache of
@@ -88,7 +91,7 @@ typedef struct stepkv_cache4 {
  * nonzero. A position outside its sequence leaves its row as it was. k_bounds
  * of the written blocks are set. STEPKV_FLAG_NONFINITE: a group held a NaN or
  * an infinity. Errors: EINVAL (null or misaligned pointers, a bad problem or
- * cache, shapes that differ), EUNSUPPORTED (d), EHIP. */
+ * cache, shapes that differ), EUNSUPPORTED (d, rows), EHIP. */
 int stepkv_cache4_compact(const stepkv_problem* pb, const stepkv_cache4* c, const void* k,
                           const void* v, const int32_t* idx, int32_t shared_idx,
                           const int32_t* cu_retained, void* stream);
@@ -110,7 +113,7 @@ int stepkv_cache4_advance(const stepkv_cache4* c, const int32_t* cu_new, void* s
  * alike; v_new likewise. k_bounds: a block whose first token is among the new
  * ones starts anew, others widen (appending the same tokens again changes
  * nothing; other values in their place leave bounds that still hold).
- * STEPKV_FLAG_NONFINITE as compact. Errors: EINVAL, EUNSUPPORTED (d), EHIP. */
+ * STEPKV_FLAG_NONFINITE as compact. Errors: EINVAL, EUNSUPPORTED (d, rows), EHIP. */
 int stepkv_cache4_append(const stepkv_cache4* c, const void* k_new, const int64_t* k_strides,
                          const void* v_new, const int64_t* v_strides, const int32_t* cu_new,
                          int32_t num_new, void* stream);
@@ -121,7 +124,7 @@ int stepkv_cache4_append(const stepkv_cache4* c, const void* k_new, const int64_
  * sequences, in the layout that stepkv_score takes. Rows at or past out_rows
  * and rows without a token are left as they were. k_out or v_out may be NULL:
  * it is not read back. Errors: EINVAL (both NULL with out_rows > 0, negative
- * out_rows, misaligned pointers), EUNSUPPORTED (d), EHIP. */
+ * out_rows, misaligned pointers), EUNSUPPORTED (d, rows), EHIP. */
 int stepkv_cache4_read(const stepkv_cache4* c, const int32_t* cu_out, int32_t out_rows,
                        void* k_out, void* v_out, void* stream);
 
@@ -146,7 +149,7 @@ size_t stepkv_cache4_decode_workspace_bytes(const stepkv_cache4* c, int32_t num_
  * A NaN in an attended key, value or query makes its results NaN. fp32 sums of
  * exact products, the probabilities in fp32. Results do
  * not depend on other sequences' contents; they are the same from call to call.
- * Errors: EINVAL, EUNSUPPORTED (d), EWORKSPACE (below
+ * Errors: EINVAL, EUNSUPPORTED (d, rows), EWORKSPACE (below
  * stepkv_cache4_decode_workspace_bytes, or not 256-byte aligned), EHIP. */
 int stepkv_cache4_decode(const stepkv_cache4* c, int32_t num_q_heads, const void* q_dec,
                          const int32_t* blocks, int32_t num_blocks, float scale, float* out,
@@ -165,7 +168,7 @@ size_t stepkv_cache4_select_workspace_bytes(const stepkv_cache4* c);
  * ascending to blocks int32 [L][S][H][num_blocks], -1 past the last; all the
  * blocks of a sequence that has no more than num_blocks.
  * Errors: EINVAL (also a cache without k_bounds, num_blocks < 1, negative
- * counts, first_blocks + last_blocks > num_blocks), EUNSUPPORTED (d),
+ * counts, first_blocks + last_blocks > num_blocks), EUNSUPPORTED (d, rows),
  * EWORKSPACE, EHIP. */
 int stepkv_cache4_select_blocks(const stepkv_cache4* c, int32_t num_q_heads, const void* q_dec,
                                 int32_t num_blocks, int32_t first_blocks, int32_t last_blocks,

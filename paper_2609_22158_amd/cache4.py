@@ -26,6 +26,7 @@ import numpy as np
 from . import binding as B
 
 BLOCK, GROUP = 64, 32  # STEPKV_CACHE4_BLOCK, STEPKV_CACHE4_GROUP
+MAX_ROWS = (1 << 30) - (1 << 20)  # STEPKV_CACHE4_MAX_ROWS
 
 _i32, _vp, _sz = ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t
 
@@ -238,6 +239,8 @@ def compact4(pb: B.Problem, cache: Cache4, k, v, idx, cu_retained, *, stream=Non
     import torch
 
     L, H, d, dev = pb.num_layers, pb.num_kv_heads, pb.head_dim, cache.device
+    if pb.cu_seqlens_dev.device != dev:
+        raise ValueError(f"pb: lies on {pb.cu_seqlens_dev.device}, the cache on {dev}")
     kp = _need(k, torch.bfloat16, (L, H, pb.ntot, d), "k", dev)
     vp = _need(v, torch.bfloat16, (L, H, pb.ntot, d), "v", dev)
     shared = idx.dim() == 1

@@ -65,6 +65,10 @@ __device__ __forceinline__ int split_rows_of(const Attend4Args& a, int s) {
   return a.blocks ? kBlock4 * min(a.nlist, (n + kBlock4 - 1) / kBlock4) : n;
 }
 
+__device__ __forceinline__ int split_rows_const(const Attend4Args& a, int held) {
+  return a.blocks ? kBlock4 * min(a.nlist, (held + kBlock4 - 1) / kBlock4) : held;
+}
+
 // Rows of a split, from the tokens there are when the kernel runs: as many as
 // give at most a.splits splits in all, sum_s ceil(n_s / rows) <= total / rows +
 // nonempty sequences. A multiple of a tile for each of the waves.
@@ -151,7 +155,7 @@ void attend4_kernel(Attend4Args a) {
   const Cache4View& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int g4 = lane >> 4, c16 = lane & 15;
-  if (blockIdx.x == 0 && tid == 0) report_rooms(c);
+  if (blockIdx.x == 0 && wave == 0) report_rooms(c);
   const int unit = uniform(blockIdx.x / a.splits);  // (layer, KV head, 16 query heads)
   const int gs = uniform(blockIdx.x - unit * a.splits);
   const int tiles = (a.G + 15) / 16;
@@ -159,7 +163,7 @@ void attend4_kernel(Attend4Args a) {
   const int l = uniform(lh / c.H), h = lh - l * c.H;
   int s = gs, w0, w1;  // this wave's rows [w0, w1) of those of its sequence
   if (a.single) {
-    const int share = (split_rows_of(a, s) + NW * kTile - 1) / (NW * kTile) * kTile;
+    const int share = (split_rows_const(a, held_const(c, s)) + NW * kTile - 1) / (NW * kTile) * kTile;
     w0 = wave * share;
     w1 = w0 + share;
   } else {
@@ -172,8 +176,7 @@ void attend4_kernel(Attend4Args a) {
     w1 = w0 + split / NW;
   }
   s = uniform(s);
-  const int held = uniform(held_tokens(c, s));
-  const int n = uniform(split_rows_of(a, s));
+  const int held = held_const(c, s), n = split_rows_const(a, held);
   const int t0 = uniform(w0 / kTile), t1 = uniform((min(n, w1) + kTile - 1) / kTile);  // its tiles
   const int heads = min(a.G - hd0, 16);
   bf16x8_t qb[NS];
@@ -189,7 +192,7 @@ void attend4_kernel(Attend4Args a) {
   f32x4_t o[NB], z = f32x4_t{};
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) o[nb] = f32x4_t{};
-  const size_t row0 = (size_t)lh * c.rows + uniform(c.cu_rows[s]);
+  const size_t row0 = (size_t)lh * c.rows + read_const(c.cu_rows, s);
   const int32_t* __restrict__ list =
       LIST ? a.blocks + (((size_t)l * c.S + s) * c.H + h) * a.nlist : nullptr;
   uint8_t* const vt = smem + wave * TB;
@@ -447,7 +450,8 @@ __global__ __launch_bounds__(THREADS) void combine4_kernel(Attend4Args a) {
     first += wave_total(
         wave_scan(s0 + lane < s ? (split_rows_of(a, s0 + lane) + split - 1) / split : 0));
   first = min(first, a.splits);
-  const int n = min((split_rows_of(a, s) + split - 1) / split, a.splits - first);
+  const int n =
+      min((split_rows_const(a, held_const(c, s)) + split - 1) / split, a.splits - first);
   const size_t stride = (size_t)per * ST;
   const float* __restrict__ base =
       a.partial + ((size_t)unit * a.splits + first) * stride + (size_t)g0 * ST;

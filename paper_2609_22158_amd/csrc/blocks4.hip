@@ -26,6 +26,10 @@ __device__ __forceinline__ int blocks_of(const Cache4View& c, int s) {
   return (held_tokens(c, s) + kBlock4 - 1) / kBlock4;
 }
 
+__device__ __forceinline__ int blocks_const(const Cache4View& c, int s) {  // of a uniform s
+  return (held_const(c, s) + kBlock4 - 1) / kBlock4;
+}
+
 // Doubles as unsigned integers in the same order; NaN as -inf, -0 as +0.
 __device__ __forceinline__ uint64_t ordered(double x) {
   if (x != x) x = -INFINITY;
@@ -137,16 +141,17 @@ __global__ __launch_bounds__(kThreads) void score4_kernel(Select4Args a) {
   const Cache4View& c = a.c;
   const int lh = uniform(blockIdx.x / a.chunks), at = uniform(blockIdx.x - lh * a.chunks);
   const int l = uniform(lh / c.H), h = lh - l * c.H;
-  int s, first;
-  locate_item(c.S, at, [&](int sq) {
+  int s = 0, first = 0;
+  if (c.S == 1 && at * kChunk >= (blocks_const(c, 0) > a.n ? blocks_const(c, 0) : 0)) return;
+  if (c.S > 1) locate_item(c.S, at, [&](int sq) {
     const int nb = blocks_of(c, sq);
     return nb > a.n ? (nb + kChunk - 1) / kChunk : 0;  // shorter ones are not ranked
   }, s, first);
   if (s < 0) return;
   const int b0 = (at - first) * kChunk;
-  const size_t base = (size_t)lh * c.nblk + c.cu_rows[s] / kBlock4 + s;
+  const size_t base = (size_t)lh * c.nblk + read_const(c.cu_rows, s) / kBlock4 + s;
   score_blocks<D, kThreads>(a.q + (((size_t)l * c.S + s) * a.Hq + h * a.G) * D, a.G,
-                            c.k_bounds + base * 2 * D, b0, min(blocks_of(c, s), b0 + kChunk),
+                            c.k_bounds + base * 2 * D, b0, min(blocks_const(c, s), b0 + kChunk),
                             a.keys + base, coef);
 }
 
@@ -163,12 +168,12 @@ __global__ __launch_bounds__(THREADS) void select4_kernel(Select4Args a) {
   const int h = uniform(blockIdx.x % c.H);
   const int s = uniform((blockIdx.x / c.H) % c.S), l = uniform(blockIdx.x / (c.H * c.S));
   int32_t* __restrict__ out = a.blocks + (size_t)blockIdx.x * a.n;
-  const int nb = uniform(blocks_of(c, s));
+  const int nb = blocks_const(c, s);
   if (nb <= a.n) {
     for (int i = tid; i < a.n; i += THREADS) out[i] = i < nb ? i : -1;
     return;
   }
-  const size_t base = (size_t)(l * c.H + h) * c.nblk + c.cu_rows[s] / kBlock4 + s;
+  const size_t base = (size_t)(l * c.H + h) * c.nblk + read_const(c.cu_rows, s) / kBlock4 + s;
   const uint64_t* keys = a.keys + base;
   // candidates [b0, b1), of which `want` are taken: those with key >> shift
   // above `bin`, and the first `ties` of those with key >> shift == bin

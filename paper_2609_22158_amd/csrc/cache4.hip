@@ -37,13 +37,6 @@ __device__ __forceinline__ uint32_t pk_sortable(uint32_t x) {
   return x ^ (__builtin_bit_cast(uint32_t, v >> 15) & 0x7fff7fffu);
 }
 
-// x[i] of an array that stays unchanged for the whole launch, read through the
-// constant address space: with a wave-uniform index the load is a scalar one,
-// which does not queue behind the rows that the compute unit streams.
-__device__ __forceinline__ int read_const(const int32_t* x, int i) {
-  return ((const __attribute__((address_space(4))) int32_t*)x)[i];
-}
-
 // Eight values of a group (the other 24 in the other lanes of the quad):
 // their codes, and the group's scale byte. With the largest magnitude
 // 1.m * 2^E in bf16 bits (E and the 7 bits of m), max <= 7 * 2^e means
@@ -115,10 +108,10 @@ __global__ __launch_bounds__(kThreads) void write4_kernel(Write4Args a) {
   __shared__ int bad_s[NWV][PR];
   const int tid = threadIdx.x;
   const Cache4View& c = a.c;
-  if (blockIdx.x == 0 && tid == 0) {
+  if (blockIdx.x == 0 && tid < kWave) {
     if (a.idx) {
       bool over = false;
-      for (int s = 0; s < c.S; ++s) {
+      for (int s = tid; s < c.S; s += kWave) {
         const int n = max(a.cu_retained[s + 1] - a.cu_retained[s], 0);
         c.lens[s] = n;
         over |= n > c.cu_rows[s + 1] - c.cu_rows[s];

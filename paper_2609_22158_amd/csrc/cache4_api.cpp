@@ -35,6 +35,7 @@ int check_cache(const stepkv_cache4* c) {
   if (!c->cu_rows_host || !c->cu_rows || !c->lens) return STEPKV_EINVAL;
   if (!offsets(c->cu_rows_host, c->num_seqs)) return STEPKV_EINVAL;
   if (c->head_dim != 64 && c->head_dim != 128) return STEPKV_EUNSUPPORTED;
+  if (c->cu_rows_host[c->num_seqs] > STEPKV_CACHE4_MAX_ROWS) return STEPKV_EUNSUPPORTED;
   if (c->cu_rows_host[c->num_seqs] > 0 &&
       (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales))
     return STEPKV_EINVAL;  // NULL buffers hold 0 rows

@@ -20,11 +20,23 @@ __device__ __forceinline__ int held_tokens(const Cache4View& c, int s) {
   return min(max(c.lens[s], 0), c.cu_rows[s + 1] - c.cu_rows[s]);
 }
 
-// Whether a sequence has more tokens than room (checked by one thread of a call).
+// x[i] of an array that stays unchanged for the whole launch, read through the
+// constant address space: with a wave-uniform index the load is a scalar one,
+// which does not queue behind the rows that the compute unit streams.
+__device__ __forceinline__ int read_const(const int32_t* x, int i) {
+  return ((const __attribute__((address_space(4))) int32_t*)x)[i];
+}
+// held_tokens of a wave-uniform sequence, where the launch does not write lens.
+__device__ __forceinline__ int held_const(const Cache4View& c, int s) {
+  return min(max(read_const(c.lens, s), 0), read_const(c.cu_rows, s + 1) - read_const(c.cu_rows, s));
+}
+
+// Reports a sequence with more tokens than room (called by one wave of a launch).
 __device__ __forceinline__ void report_rooms(const Cache4View& c) {
   if (c.status == nullptr) return;
   bool over = false;
-  for (int s = 0; s < c.S; ++s) over |= c.lens[s] > c.cu_rows[s + 1] - c.cu_rows[s];
+  for (int s = threadIdx.x & 63; s < c.S; s += kWave)
+    over |= c.lens[s] > c.cu_rows[s + 1] - c.cu_rows[s];
   if (over) atomicOr(c.status, kFlagOutRows4);
 }
 

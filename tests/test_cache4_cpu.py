@@ -185,6 +185,14 @@ def test_refuses_arguments(lib, call, kw, code):
     assert CALLS[call](lib, ctypes.byref(_cache()), **kw) == code
 
 
+def test_refuses_rows_past_the_limit(lib):
+    c = _cache(rooms=(C4.MAX_ROWS,))
+    assert lib.stepkv_cache4_select_workspace_bytes(ctypes.byref(c)) > 0
+    c = _cache(rooms=(C4.MAX_ROWS, 1))
+    assert CALLS["advance"](lib, ctypes.byref(c)) == B.EUNSUPPORTED
+    assert lib.stepkv_cache4_decode_workspace_bytes(ctypes.byref(c), 8, 0) == 0
+
+
 def test_selection_needs_bounds(lib):
     c = ctypes.byref(_cache(k_bounds=None))
     assert CALLS["select"](lib, c) == B.EINVAL and CALLS["sparse"](lib, c) == B.EINVAL

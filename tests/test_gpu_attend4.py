@@ -108,8 +108,15 @@ CASES = {
     # more splits than one pass of lanes merges, and 70 sequences
     "long_d64": (1, 2, 1, 64, [40001], [40001]),
     "many_seqs": (1, 2, 2, 64, [(37 * i) % 300 for i in range(70)], [300] * 70),
+    # more sequences than a wave, or a workgroup, has lanes: many short ones and a long one among them
+    "thousands": (1, 4, 2, 64, [3 + i % 5 if i != 1500 else 2500 for i in range(3000)],
+                  [8 if i != 1500 else 2600 for i in range(3000)]),
     # enough (layer, head) pairs that a split is longer than a tile per wave
     "wide": (16, 16, 16, 64, [1025, 2100], [1025, 2200]),
+    "wide_d128": (8, 8, 8, 128, [1700, 40, 900, 1, 0, 64, 333, 2000], [1700, 50, 900, 1, 9, 64, 400, 2000]),
+    # as many, of one split each
+    "wide_short": (16, 16, 16, 64, [1025, 900], [1025, 1000]),
+    "wide_short_d128": (8, 16, 8, 128, [600, 1, 0, 64, 333], [600, 1, 5, 64, 400]),
 }
 
 
@@ -165,7 +172,7 @@ def test_not_a_number(gpu_lib):
     assert torch.isfinite(out[0, :2]).all()
 
 
-@pytest.mark.parametrize("cid", ["g7_splits", "lengths_d64", "g20_two_tiles", "many_seqs", "long_d64"])
+@pytest.mark.parametrize("cid", ["g7_splits", "lengths_d64", "g20_two_tiles", "many_seqs", "long_d64", "wide_short_d128"])
 def test_decode_over_listed_blocks(cid, gpu_lib):
     """Lists of any blocks, one per (layer, sequence, KV head), with entries that are passed over:
     -1, ids that are no block of the sequence, repeats and entries out of order."""
@@ -228,6 +235,44 @@ def test_select_and_sparse_decode(cid, gpu_lib):
         assert torch.equal(out, o2) and torch.equal(lse, l2)
         if n in (1, 20, 2000):
             m.check(out, lse, blocks=taken)
+    log(f"[select4 {cid}] ok")
+
+
+SELECT_MANY = {
+    # name: (L, H, G, d, tokens): the ways of sharing out the scores
+    "alone_small_groups": (8, 8, 3, 64, [4000, 64 * 130, 64, 0, 700, 6000, 1, 9999]),
+    "alone_wide": (16, 16, 1, 128, [70000, 12345]),
+    "spread": (2, 3, 5, 128, [64 * 3000, 50000]),
+    "spread_past_lds": (1, 2, 2, 64, [64 * 9000 - 1, 64 * 5000, 3]),
+}
+
+
+@pytest.mark.parametrize("cid", list(SELECT_MANY))
+def test_select_many(cid, gpu_lib):
+    """Selections of many blocks and rows against scores in 64 bits from the same bounds."""
+    import torch
+
+    L, H, G, d, lens = SELECT_MANY[cid]
+    S = len(lens)
+    cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(9)
+    x = torch.randn((L, H, int(cu[-1]) // 64 + S, 2, d), generator=gen, device="cuda")
+    bounds = x.sort(dim=3).values.bfloat16()
+    # buffers of no rows would do: the selection reads lens and bounds alone
+    cache = C4.Cache4(L, H, d, cu, k_bounds=bounds, lens=torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    q = torch.randn((L, S, H * G, d), generator=gen, device="cuda").bfloat16()
+    for n, first, last in ((7, 1, 1), (100, 0, 2)):
+        got = C4.select_blocks4(cache, q, n, first=first, last=last).cpu().numpy()
+        for s in range(S):
+            nb, at = -(-lens[s] // 64), int(cu[s]) // 64 + s
+            qs = q[:, s].double().view(L, H, G, 1, d)
+            b = bounds[:, :, None, at:at + nb].double()
+            score = torch.maximum(qs * b[..., 0, :], qs * b[..., 1, :]).sum(dim=(2, 4)).cpu().numpy()
+            for l in range(L):
+                for h in range(H):
+                    want = R.select_blocks(score[l, h], n, first, last)
+                    assert np.array_equal(got[l, s, h], want), (cid, n, l, s, h)
     log(f"[select4 {cid}] ok")
 
 
