@@ -75,7 +75,7 @@ Cache4View view(const stepkv_cache4* c) {
 }
 
 // A launch has at most 2^31 - 1 workgroups.
-bool grid_fits(int64_t workgroups) { return workgroups <= std::numeric_limits<int32_t>::max(); }
+bool grid_fits(int64_t workgroups) { return workgroups <= std::numeric_limits<int32_t>::max() - 8; }
 
 Attend4Args attend_args(const stepkv_cache4* c, int32_t num_q_heads, int32_t num_blocks) {
   Attend4Args a{};
