@@ -20,9 +20,9 @@
 //  - V: lane l converts 32 channels (one scale) of one row to bf16 and puts
 //    them into the wave's LDS tile; ds_read_b64_tr_b16 gives them back as the
 //    B operand, a column's 4 + 4 rows per lane in the order in which the lane
-//    holds P. P is the A operand, as three bf16 parts that are it exactly; the
-//    same parts times ones give the softmax's sum on the matrix cores, which
-//    are busy a third of the time.
+//    holds P. P is the A operand, as three bf16 parts that are it exactly (in
+//    one operand for narrow groups); the same parts times ones give the
+//    softmax's sum on the matrix cores, which have the time.
 // The next tile is loaded where the registers of a tile are free, before its
 // softmax and P V. A second set of registers, loaded a tile earlier, costs a
 // wave per SIMD and is no faster (8 layers x 8 heads x 131071 rows, splits of
@@ -106,27 +106,44 @@ __device__ __forceinline__ int v_read(int r, int j, int gp, int c) {
 
 typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
 
-// Eight probabilities as three bf16 operands whose sum they are, exactly: 8
-// bits of the significand each, by truncation (the rest is exact in fp32).
+// Eight probabilities as bf16 operands whose sum they are, exactly: three parts
+// of 8 bits of the significand each, by truncation (the rest is exact in fp32).
+// Groups of at most 5 heads lie in the operand's 16 rows three times (C = 3), and
+// each copy takes its own part: one product instead of three (8 layers x 8 heads
+// x 131071 rows, G 4: 200 -> 187 us; two copies of at most 8 heads and two
+// products: no faster).
+template <int C>
 struct Parts {
-  bf16x8_t x[3];
+  static constexpr int N = 3 / C;
+  bf16x8_t x[N];
 };
-__device__ __forceinline__ Parts split3(const float (&p)[8]) {
-  u32x4_t w[3];
+__device__ __forceinline__ uint32_t upper(uint32_t b, uint32_t a) {  // the upper halves of a, b
+  return __builtin_amdgcn_perm(b, a, 0x07060302u);
+}
+// x less its bits in mask (the upper half, or none).
+__device__ __forceinline__ uint32_t below(uint32_t x, uint32_t mask) {
+  return __float_as_uint(__uint_as_float(x) - __uint_as_float(x & mask));
+}
+template <int C>
+__device__ __forceinline__ Parts<C> split_parts(const float (&p)[8], int copy) {
+  constexpr uint32_t F = 0xffff0000u;
+  const uint32_t m1 = copy >= 1 ? F : 0u, m2 = copy >= 2 ? F : 0u;
+  u32x4_t w[Parts<C>::N];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    uint32_t a = __float_as_uint(p[2 * i]), b = __float_as_uint(p[2 * i + 1]);
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      w[k][i] = __builtin_amdgcn_perm(b, a, 0x07060302u);  // the upper halves
-      if (k == 2) break;
-      a = __float_as_uint(__uint_as_float(a) - __uint_as_float(a & 0xffff0000u));
-      b = __float_as_uint(__uint_as_float(b) - __uint_as_float(b & 0xffff0000u));
+    const uint32_t a = __float_as_uint(p[2 * i]), b = __float_as_uint(p[2 * i + 1]);
+    if constexpr (C == 3) {
+      w[0][i] = upper(below(below(b, m1), m2), below(below(a, m1), m2));
+    } else {
+      const uint32_t a1 = below(a, F), b1 = below(b, F);
+      w[0][i] = upper(b, a);
+      w[1][i] = upper(b1, a1);
+      w[2][i] = upper(below(b1, F), below(a1, F));
     }
   }
-  Parts r;
+  Parts<C> r;
 #pragma unroll
-  for (int k = 0; k < 3; ++k) r.x[k] = __builtin_bit_cast(bf16x8_t, w[k]);
+  for (int k = 0; k < Parts<C>::N; ++k) r.x[k] = __builtin_bit_cast(bf16x8_t, w[k]);
   return r;
 }
 
@@ -137,8 +154,9 @@ __device__ __forceinline__ void finish(const Attend4Args& a, size_t row, int ch,
   if (a.lse && ch == 0) a.lse[row] = Z == 0.f ? -INFINITY : (M + log2f(Z)) * 0.693147180559945309f;
 }
 
-// NW waves share a split (or, with a.single, a whole sequence).
-template <int D, int NW, bool LIST>
+// NW waves share a split (or, with a.single, a whole sequence); C copies (1 or 3)
+// of the query heads in the operands' rows.
+template <int D, int NW, bool LIST, int C>
 __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(LIST && D == 128 ? 3 : 4)))
 void attend4_kernel(Attend4Args a) {
   constexpr int NS = D / kGroup4;    // scales a row; MFMA steps of S
@@ -184,13 +202,15 @@ void attend4_kernel(Attend4Args a) {
   const int held = held_const(c, s), n = split_rows_const(a, held);
   const int t0 = uniform(w0 / kTile), t1 = uniform((min(n, w1) + kTile - 1) / kTile);  // its tiles
   const int heads = min(a.G - hd0, 16);
+  constexpr int kCols = 16 / C;  // columns of a copy
+  const int copy = c16 / kCols, hcol = c16 % kCols;
   bf16x8_t qb[NS];
 #pragma unroll
   for (int ks = 0; ks < NS; ++ks) {
     qb[ks] = bf16x8_t{};
-    if (c16 < heads)
+    if (hcol < heads && copy < C)
       qb[ks] = *reinterpret_cast<const bf16x8_t*>(
-          a.q + (((size_t)l * c.S + s) * a.Hq + h * a.G + hd0 + c16) * D + D / 4 * g4 + 8 * ks);
+          a.q + (((size_t)l * c.S + s) * a.Hq + h * a.G + hd0 + hcol) * D + D / 4 * g4 + 8 * ks);
   }
   const float cl2 = a.scale * kLog2e;
   float m_ref = -INFINITY;
@@ -346,10 +366,10 @@ void attend4_kernel(Attend4Args a) {
     float p[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) p[i] = fast_exp2(fmaf(y[i], cl2, -m));
-    const Parts pp = split3(p);
+    const Parts<C> pp = split_parts<C>(p, copy);
     const bf16x8_t one = __builtin_bit_cast(bf16x8_t, u32x4_t{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
 #pragma unroll
-    for (int k = 0; k < 3; ++k) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pp.x[k], one, z, 0, 0, 0);
+    for (int k = 0; k < Parts<C>::N; ++k) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pp.x[k], one, z, 0, 0, 0);
     constexpr int kOps = 2;  // column blocks at a time (4: as fast, but 6 registers more)
 #pragma unroll
     for (int nb0 = 0; nb0 < NB; nb0 += kOps) {
@@ -366,7 +386,7 @@ void attend4_kernel(Attend4Args a) {
                                    __builtin_shufflevector(b[0], b[1], 0, 1, 2, 3, 4, 5, 6, 7));
       }
 #pragma unroll
-      for (int k = 0; k < 3; ++k)
+      for (int k = 0; k < Parts<C>::N; ++k)
 #pragma unroll
         for (int i = 0; i < kOps; ++i)
           o[nb0 + i] =
@@ -388,7 +408,7 @@ void attend4_kernel(Attend4Args a) {
   auto state = reinterpret_cast<float(*)[16][ST]>(smem);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (4 * g4 + i < heads) {
+    if ((4 * g4 + i) % kCols < heads && (4 * g4 + i) / kCols < C) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -398,7 +418,7 @@ void attend4_kernel(Attend4Args a) {
       if (c16 == 0) state[wave][4 * g4 + i][D + 1] = z[i];
     }
   }
-  if (g4 == 0 && c16 < heads) state[wave][c16][D] = m_ref;
+  if (g4 == 0 && c16 < heads) state[wave][c16][D] = m_ref;  // the same in every copy
   __syncthreads();
   float* const part = a.partial + ((size_t)unit * a.splits + gs) * min(a.G, 16) * ST;
   const size_t row_out = ((size_t)l * c.S + s) * a.Hq + h * a.G + hd0;
@@ -412,8 +432,14 @@ void attend4_kernel(Attend4Args a) {
     for (int w = 0; w < NW; ++w) {
       const float m = state[w][hd][D];
       const float x = m == -INFINITY ? 0.f : fast_exp2(m - M);  // a NaN sum stays NaN
-      Z = fmaf(state[w][hd][D + 1], x, Z);
-      O = fmaf(state[w][hd][ch], x, O);
+      float z1 = state[w][hd][D + 1], o1 = state[w][hd][ch];
+#pragma unroll
+      for (int k = 1; k < C; ++k) {
+        z1 += state[w][k * kCols + hd][D + 1];
+        o1 += state[w][k * kCols + hd][ch];
+      }
+      Z = fmaf(z1, x, Z);
+      O = fmaf(o1, x, O);
     }
     if (a.single) {
       finish(a, row_out + hd, ch, D, M, Z, O);
@@ -563,12 +589,16 @@ template <int D>
 void launch_attend(const Attend4Args& a, hipStream_t st) {
   const unsigned units = (unsigned)(a.c.L * a.c.H) * (unsigned)((a.G + 15) / 16);
   const dim3 grid((units * (unsigned)a.splits + 7u) / 8u * 8u);
-  auto run = [&](auto nw) {
-    constexpr int NW = decltype(nw)::value;
+  auto copies = [&](auto nw, auto cc) {
+    constexpr int NW = decltype(nw)::value, C = decltype(cc)::value;
     if (a.blocks)
-      hipLaunchKernelGGL((attend4_kernel<D, NW, true>), grid, dim3(NW * kWave), 0, st, a);
+      hipLaunchKernelGGL((attend4_kernel<D, NW, true, C>), grid, dim3(NW * kWave), 0, st, a);
     else
-      hipLaunchKernelGGL((attend4_kernel<D, NW, false>), grid, dim3(NW * kWave), 0, st, a);
+      hipLaunchKernelGGL((attend4_kernel<D, NW, false, C>), grid, dim3(NW * kWave), 0, st, a);
+  };
+  auto run = [&](auto nw) {
+    if (a.G <= 5) copies(nw, std::integral_constant<int, 3>{});
+    else copies(nw, std::integral_constant<int, 1>{});
   };
   if (a.single && grid.x <= 256) run(std::integral_constant<int, 8>{});
   else run(std::integral_constant<int, kWaves>{});

@@ -94,6 +94,8 @@ CASES = {
     "lengths_d64": (2, 4, 1, 64, [1, 0, 31, 32, 33, 95, 96, 97, 511, 512, 513],
                     [1, 0, 31, 64, 33, 95, 96, 120, 511, 700, 513]),
     "g1": (2, 3, 3, 128, [700, 65], [700, 100]),
+    "g5": (1, 10, 2, 128, [1333, 40], [1333, 40]),
+    "g6_d64": (1, 12, 2, 64, [1400, 33], [1500, 33]),
     "g7_splits": (1, 14, 2, 128, [2560, 31, 900, 1300], [4000, 31, 901, 1400]),
     "g8_d64": (2, 16, 2, 64, [1100, 17, 16], [1100, 17, 20]),
     "g12": (1, 24, 2, 128, [530, 47], [600, 50]),
