@@ -147,8 +147,9 @@ size_t stepkv_cache4_decode_workspace_bytes(const stepkv_cache4* c, int32_t num_
  * not above every entry before it, is passed over, and so are the entries past
  * as many as the sequence has blocks.
  * A NaN in an attended key, value or query makes its results NaN. fp32 sums of
- * exact products, the probabilities in fp32. Results do
- * not depend on other sequences' contents; they are the same from call to call.
+ * exact products, the probabilities in fp32. Results are
+ * the same from call to call and do not depend on what other sequences hold;
+ * their lengths may move the borders of the splits, and so the last bits.
  * Errors: EINVAL, EUNSUPPORTED (d, rows), EWORKSPACE (below
  * stepkv_cache4_decode_workspace_bytes, or not 256-byte aligned), EHIP. */
 int stepkv_cache4_decode(const stepkv_cache4* c, int32_t num_q_heads, const void* q_dec,

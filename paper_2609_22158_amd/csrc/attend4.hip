@@ -456,7 +456,9 @@ void attend4_kernel(Attend4Args a) {
 // out and lse of a (layer, sequence, KV head, 16 query heads), or of one query
 // head of them: the splits' states merged by a running maximum, four in flight
 // per thread. A thread per (head, channel), or with one head a group of
-// THREADS / D threads per channel over the splits, merged in order.
+// THREADS / D threads per channel over the splits, merged in order. Two waits for
+// memory bound it: 4 us for 64 heads of 33 splits each, 11 for 1792 x 7 heads of
+// one or two.
 template <int D, int THREADS, bool ONE>
 __global__ __launch_bounds__(THREADS) void combine4_kernel(Attend4Args a) {
   constexpr int ST = D + 2;

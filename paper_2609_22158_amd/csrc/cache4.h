@@ -31,8 +31,8 @@ struct Write4Args {
   const uint16_t* v;
   int64_t k_layer, k_row, k_head, v_layer, v_row, v_head;
   const int32_t* cu_src;     // compact: cu_seqlens; append: cu_new
-  const int32_t* cu_retained;// compact only
-  const int32_t* idx;        // compact: [L*H][nsrc] or [nsrc]; append: null
+  const int32_t* cu_retained;// compact; append: null
+  const int32_t* idx;        // compact: [L*H][nsrc] or [nsrc]
   int nsrc;                  // source rows (Ntot, num_new)
   int shared_idx;
   int nblocks;               // (sequence, block) pairs a (layer, head) can touch

@@ -158,8 +158,9 @@ int stepkv_cache4_compact(const stepkv_problem* pb, const stepkv_cache4* c, cons
       pb->head_dim != c->head_dim || pb->num_seqs != c->num_seqs || !pb->cu_seqlens_host ||
       !pb->cu_seqlens || !offsets(pb->cu_seqlens_host, pb->num_seqs))
     return STEPKV_EINVAL;
-  if (!k || !v || !idx || !cu_retained || !aligned(k, 16) || !aligned(v, 16))
-    return STEPKV_EINVAL;
+  if (!cu_retained || !aligned(k, 16) || !aligned(v, 16)) return STEPKV_EINVAL;
+  if (pb->cu_seqlens_host[pb->num_seqs] > 0 && (!k || !v || !idx))
+    return STEPKV_EINVAL;  // NULL sources hold 0 tokens
   Write4Args a;
   a.c = view(c);
   a.k = static_cast<const uint16_t*>(k);

@@ -175,6 +175,39 @@ def test_compact_without_room_and_with_bad_positions(gpu_lib):
     assert np.array_equal(got[1, 1, a:a + 60], R.dequantise4(*R.quantise4(want_k[1, 1, 2][:60])))
 
 
+def test_compact_from_no_tokens(gpu_lib):
+    """A source without a token empties the cache's sequences; reads of them give nothing."""
+    import torch
+
+    cache = filled(C4.Cache4(1, 2, 64, [0, 8, 16]))
+    cache.lens.fill_(5)
+    pb = B.Problem(1, 2, 2, 64, 1, np.zeros(3, np.int32), np.zeros(3, np.int32))
+    none = torch.empty((1, 2, 0, 64), dtype=torch.bfloat16, device="cuda")
+    cu = torch.zeros(3, dtype=torch.int32, device="cuda")
+    C4.compact4(pb, cache, none, none, torch.empty((1, 2, 0), dtype=torch.int32, device="cuda"), cu)
+    assert cache.lens.tolist() == [0, 0]
+    check_rows(cache, {}, {}, [0, 8])
+    q = torch.ones((1, 2, 2, 64), dtype=torch.bfloat16, device="cuda")
+    out, blocks, lse = C4.decode_sparse4(cache, q, 3, want_lse=True)
+    assert (out == 0).all() and (blocks == -1).all() and (lse == -np.inf).all()
+
+
+def test_append_past_a_full_room(gpu_lib):
+    """New tokens that lie past the room altogether write nothing, whatever block they would be in."""
+    import torch
+
+    cache = filled(C4.Cache4(1, 1, 64, [0, 66]))
+    t = B.bf16_from_bits(bf16(np.random.default_rng(8), (1, 80, 1, 64)))
+    first = torch.tensor([0, 66], dtype=torch.int32, device="cuda")
+    C4.advance4(cache, first)
+    C4.append4(cache, t[:, :66], t[:, :66], first)
+    before = [x for x in host(cache)]
+    cache.lens.fill_(80)
+    C4.append4(cache, t[:, 70:], t[:, 70:], torch.tensor([0, 10], dtype=torch.int32, device="cuda"))
+    assert all(np.array_equal(x, y) for x, y in zip(before, host(cache)))
+    assert cache.status() == B.FLAG_OUT_ROWS
+
+
 def test_values_at_the_edges(gpu_lib):
     """NaN, infinities, zeros, signed zeros, the largest and the smallest magnitudes, ties."""
     import torch
