@@ -129,7 +129,8 @@ int stepkv_cache4_read(const stepkv_cache4* c, const int32_t* cu_out, int32_t ou
                        void* k_out, void* v_out, void* stream);
 
 /* Bytes of device workspace stepkv_cache4_decode needs for num_q_heads query
- * heads (0 when invalid); num_blocks as the call's, 0 without a list. */
+ * heads (0 when invalid); num_blocks as the call's, 0 without a list. 256: the
+ * call needs none, and takes NULL (short sequences, which are not split). */
 size_t stepkv_cache4_decode_workspace_bytes(const stepkv_cache4* c, int32_t num_q_heads,
                                             int32_t num_blocks);
 

@@ -223,7 +223,12 @@ def _workspace(workspace, cache, stream, size, *args):
         key = (size, args)
         nbytes = cache._sizes.get(key)
         if nbytes is None:
-            nbytes = cache._sizes[key] = max(int(_fns[size](cache._ref, *args)), 1)
+            nbytes = int(_fns[size](cache._ref, *args))
+            if size == "stepkv_cache4_decode_workspace_bytes" and nbytes <= 256:
+                nbytes = 0  # none is needed
+            cache._sizes[key] = nbytes
+        if nbytes == 0:
+            return None, None, 0
         workspace = _empty((nbytes,), torch.uint8, cache, stream)
         return workspace, workspace.data_ptr(), nbytes
     if workspace.device != cache.device or not workspace.is_contiguous():

@@ -112,18 +112,22 @@ int check_select(const stepkv_cache4* c, int32_t num_q_heads, const void* q_dec,
   return STEPKV_OK;
 }
 
-int run_attend(const stepkv_cache4* c, int32_t num_q_heads, const void* q_dec,
-               const int32_t* blocks, int32_t num_blocks, float scale, float* out, float* lse,
-               void* workspace, hipStream_t st) {
-  Attend4Args a = attend_args(c, num_q_heads, num_blocks);
+size_t partial_bytes(const Attend4Args& a) {
+  return align_up(sizeof(float) * attend4_partial_floats(a));
+}
+
+bool attend_fits(const Attend4Args& a) {
+  return grid_fits((int64_t)a.c.L * a.c.H * ((a.G + 15) / 16) * a.splits);
+}
+
+int run_attend(const stepkv_cache4* c, Attend4Args a, const void* q_dec, const int32_t* blocks,
+               float scale, float* out, float* lse, void* workspace, hipStream_t st) {
   a.q = static_cast<const uint16_t*>(q_dec);
   a.blocks = blocks;
   a.out = out;
   a.lse = lse;
   a.partial = static_cast<float*>(workspace);
   a.scale = scale > 0.0f ? scale : (float)(1.0 / std::sqrt((double)c->head_dim));
-  const int64_t lh = (int64_t)c->num_layers * c->num_kv_heads;
-  if (!grid_fits(lh * ((a.G + 15) / 16) * a.splits)) return STEPKV_EUNSUPPORTED;
   return hip_status(launch_attend4(a, st));
 }
 
@@ -247,8 +251,7 @@ size_t stepkv_cache4_decode_workspace_bytes(const stepkv_cache4* c, int32_t num_
                                             int32_t num_blocks) {
   if (check_cache(c) != STEPKV_OK || check_heads(c, num_q_heads) != STEPKV_OK || num_blocks < 0)
     return 0;
-  const Attend4Args a = attend_args(c, num_q_heads, num_blocks);
-  return std::max(align_up(sizeof(float) * attend4_partial_floats(a)), kAlign);
+  return std::max(partial_bytes(attend_args(c, num_q_heads, num_blocks)), kAlign);
 }
 
 int stepkv_cache4_decode(const stepkv_cache4* c, int32_t num_q_heads, const void* q_dec,
@@ -258,10 +261,12 @@ int stepkv_cache4_decode(const stepkv_cache4* c, int32_t num_q_heads, const void
   if (rc == STEPKV_OK) rc = check_attend(c, num_q_heads, q_dec, scale, out);
   if (rc != STEPKV_OK) return rc;
   if (blocks ? num_blocks < 1 : num_blocks != 0) return STEPKV_EINVAL;
-  if (!workspace || !aligned(workspace, kAlign) ||
-      ws_bytes < stepkv_cache4_decode_workspace_bytes(c, num_q_heads, num_blocks))
+  const Attend4Args a = attend_args(c, num_q_heads, num_blocks);
+  if (!attend_fits(a)) return STEPKV_EUNSUPPORTED;
+  const size_t need = partial_bytes(a);
+  if (need > 0 && (!workspace || !aligned(workspace, kAlign) || ws_bytes < need))
     return STEPKV_EWORKSPACE;
-  return run_attend(c, num_q_heads, q_dec, blocks, num_blocks, scale, out, lse, workspace,
+  return run_attend(c, a, q_dec, blocks, scale, out, lse, workspace,
                     static_cast<hipStream_t>(stream));
 }
 
@@ -300,15 +305,16 @@ int stepkv_cache4_decode_sparse(const stepkv_cache4* c, int32_t num_q_heads, con
   if (rc == STEPKV_OK)
     rc = check_select(c, num_q_heads, q_dec, num_blocks, first_blocks, last_blocks, blocks);
   if (rc != STEPKV_OK) return rc;
-  if (!workspace || !aligned(workspace, kAlign) ||
-      ws_bytes < stepkv_cache4_sparse_workspace_bytes(c, num_q_heads, num_blocks))
+  const Attend4Args a = attend_args(c, num_q_heads, num_blocks);
+  if (!attend_fits(a)) return STEPKV_EUNSUPPORTED;
+  const size_t keys = keys_bytes(c);
+  if (!workspace || !aligned(workspace, kAlign) || ws_bytes < keys + partial_bytes(a))
     return STEPKV_EWORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   rc = run_select(c, num_q_heads, q_dec, num_blocks, first_blocks, last_blocks, blocks, ws, st);
   if (rc != STEPKV_OK) return rc;
-  return run_attend(c, num_q_heads, q_dec, blocks, num_blocks, scale, out, lse,
-                    ws + keys_bytes(c), st);
+  return run_attend(c, a, q_dec, blocks, scale, out, lse, ws + keys, st);
 }
 
 }  // extern "C"

@@ -214,6 +214,8 @@ def test_workspace_sizes(lib):
     assert lib.stepkv_cache4_decode_workspace_bytes(c, 8, -1) == 0
     assert lib.stepkv_cache4_sparse_workspace_bytes(c, 8, 0) == 0
     assert lib.stepkv_cache4_select_workspace_bytes(ctypes.byref(_cache(head_dim=96))) == 0
+    # short sequences need none: the smallest size says so
+    assert lib.stepkv_cache4_decode_workspace_bytes(ctypes.byref(_cache(rooms=(64, 300))), 8, 0) == 256
     # a cache without room still has a workspace to pass
     assert lib.stepkv_cache4_decode_workspace_bytes(ctypes.byref(_cache(rooms=(0, 0))), 8, 0) >= 256
 
