@@ -357,14 +357,16 @@ def _results(cache, Hq, out, lse, want_lse, stream):
 def decode_attention4(cache: Cache4, q_dec, *, blocks=None, scale: float = 0.0, out=None, lse=None,
                       want_lse: bool = False, workspace=None, stream=None):
     """stepkv_cache4_decode: fp32 [L][S][Hq][d], over all tokens or the listed blocks (int32
-    [L][S][Hkv][n], as select_blocks4 gives them). With ``want_lse`` or an ``lse`` buffer also
+    [L][S][Hkv][n], n >= 1, as select_blocks4 gives them). With ``want_lse`` or an ``lse`` buffer also
     the rows' natural-log log-sum-exps [L][S][Hq]: (out, lse)."""
     import torch
 
     qp, Hq = _queries(cache, q_dec)
     bp, n = None, 0
     if blocks is not None:
-        n = int(blocks.shape[-1])
+        n = int(blocks.shape[-1]) if blocks.dim() else 0
+        if n < 1:  # the library takes a null list for none, which attends to every token
+            raise ValueError("blocks: a list of one block at least")
         bp = _need(blocks, torch.int32, (cache.num_layers, cache.num_seqs, cache.num_kv_heads, n),
                    "blocks", cache.device)
     out, op, lse, lp = _results(cache, Hq, out, lse, want_lse, stream)
