@@ -90,7 +90,8 @@ def load() -> ctypes.CDLL:
 
 # ---------------------------------------------------------------- the cache
 class Cache4:
-    """A 4-bit cache of S sequences: sequence s may use rows cu_rows[s] .. cu_rows[s + 1] - 1.
+    """A 4-bit cache of S sequences: sequence s may use rows cu_rows[s] .. cu_rows[s + 1] - 1
+    (copied: what is written into the given array later changes nothing).
 
     The buffers are allocated (zeroed) unless given; ``k_bounds=False`` keeps no bounds, for
     caches whose blocks are never selected. ``lens`` (int32 [S]) counts each sequence's tokens."""
@@ -101,7 +102,8 @@ class Cache4:
         import torch
 
         self.num_layers, self.num_kv_heads, self.head_dim = num_layers, num_kv_heads, head_dim
-        self.cu_rows = np.ascontiguousarray(cu_rows, dtype=np.int32)
+        self.cu_rows = np.array(cu_rows, dtype=np.int32, order="C")  # a copy: the library reads it at every call
+        self.cu_rows.setflags(write=False)
         if self.cu_rows.ndim != 1 or self.cu_rows.size < 2:
             raise ValueError("cu_rows: the row offsets of one sequence or more")
         self.num_seqs = int(self.cu_rows.size - 1)
@@ -110,7 +112,7 @@ class Cache4:
         L, H, R, S, d, dev = (num_layers, num_kv_heads, self.rows, self.num_seqs, head_dim,
                               self.device)
         self.num_bounds = R // BLOCK + S
-        self.cu_rows_dev = torch.from_numpy(self.cu_rows).to(dev)
+        self.cu_rows_dev = torch.tensor(self.cu_rows, device=dev)
 
         def buffer(t, dtype, shape, name):
             if t is None:
