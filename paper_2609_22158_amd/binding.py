@@ -361,11 +361,14 @@ class Problem:
                  window: int, cu_seqlens, cu_steps, device="cuda", status: bool = True):
         import torch
 
-        self.cu_seqlens = np.ascontiguousarray(cu_seqlens, dtype=np.int32)
-        self.cu_steps = np.ascontiguousarray(cu_steps, dtype=np.int32)
+        # copies: the library reads them at every call
+        self.cu_seqlens = np.array(cu_seqlens, dtype=np.int32, order="C")
+        self.cu_steps = np.array(cu_steps, dtype=np.int32, order="C")
+        self.cu_seqlens.setflags(write=False)
+        self.cu_steps.setflags(write=False)
         self.num_seqs = int(self.cu_seqlens.shape[0] - 1)
-        self.cu_seqlens_dev = torch.from_numpy(self.cu_seqlens).to(device)
-        self.cu_steps_dev = torch.from_numpy(self.cu_steps).to(device)
+        self.cu_seqlens_dev = torch.tensor(self.cu_seqlens, device=device)
+        self.cu_steps_dev = torch.tensor(self.cu_steps, device=device)
         self.num_layers, self.num_q_heads, self.num_kv_heads = num_layers, num_q_heads, num_kv_heads
         self.head_dim, self.window = head_dim, window
         self.device = device
