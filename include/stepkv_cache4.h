@@ -41,7 +41,10 @@
  * Sequence s owns rows cu_rows[s] .. cu_rows[s+1] - 1 (its room) and holds
  * lens[s] tokens, token j in row cu_rows[s] + j. lens[s] may exceed the room:
  * tokens past it are neither stored nor read, and calls that write or attend
- * set STEPKV_FLAG_OUT_ROWS. Rows that hold no token are never read or written.
+ * set STEPKV_FLAG_OUT_ROWS. So does a writing call for a token of its span that
+ * has no source (a compacted position outside its sequence, a new token at or
+ * past num_new): such a token keeps what its row holds, and counts as that.
+ * Rows that hold no token are never read or written.
  * Block b of sequence s is its tokens 64 b .. 64 b + 63; k_bounds holds the
  * least (0) and greatest (1) key value per channel over the tokens that the
  * block holds (NaN where one is NaN), at block floor(cu_rows[s]/64) + s + b.
@@ -88,10 +91,11 @@ typedef struct stepkv_cache4 {
  * lens[s] = R_s. pb gives the source (num_layers, num_kv_heads, head_dim and
  * num_seqs as the cache's); k, v, idx and cu_retained are as stepkv_compact's,
  * and idx is int32 [Ntot], one set for every layer and head, if shared_idx is
- * nonzero. A position outside its sequence leaves its row as it was. k_bounds
- * of the written blocks are set. STEPKV_FLAG_NONFINITE: a group held a NaN or
- * an infinity. Errors: EINVAL (null or misaligned pointers, a bad problem or
- * cache, shapes that differ), EUNSUPPORTED (d, rows), EHIP. */
+ * nonzero. A position outside its sequence leaves its row as it was
+ * (STEPKV_FLAG_OUT_ROWS). k_bounds of the R_s tokens' blocks are set.
+ * STEPKV_FLAG_NONFINITE: a group held a NaN or an infinity. Errors: EINVAL (null
+ * or misaligned pointers, a bad problem or cache, shapes that differ),
+ * EUNSUPPORTED (d, rows), EHIP. */
 int stepkv_cache4_compact(const stepkv_problem* pb, const stepkv_cache4* c, const void* k,
                           const void* v, const int32_t* idx, int32_t shared_idx,
                           const int32_t* cu_retained, void* stream);
@@ -105,8 +109,9 @@ int stepkv_cache4_advance(const stepkv_cache4* c, const int32_t* cu_new, void* s
  * cu_new[s] .. cu_new[s+1] - 1 of k_new and v_new become the last
  * n_s = cu_new[s+1] - cu_new[s] tokens of sequence s, lens[s] - n_s ..
  * lens[s] - 1. num_new is the number of tokens that k_new and v_new hold (host;
- * tokens at or past it are not read); n_s may be zero. Token t of layer l and
- * head h is the d contiguous bf16 values at
+ * tokens at or past it are not read: their rows stay as they were, and
+ * STEPKV_FLAG_OUT_ROWS is set; with num_new 0 nothing is done at all); n_s may
+ * be zero. Token t of layer l and head h is the d contiguous bf16 values at
  *   k_new + l * k_strides[0] + t * k_strides[1] + h * k_strides[2]
  * (strides in elements, multiples of 8, host int64 [3]; k_new 16-byte
  * aligned), so token-major and head-major tensors and slices of them serve

@@ -94,13 +94,120 @@ __device__ __forceinline__ void span_const(const Write4Args& a, int s, int& j0, 
   }
 }
 
+// A block of 64 tokens that a call's spans touch, and the span of its sequence.
+struct Block4 {
+  int s, blk, j0, j1, src0, src1, row0;
+};
+
+// Block `at` of those that the spans touch, in the order of the sequences; false
+// past the last. Wave-uniform.
+__device__ __forceinline__ bool find_block(const Write4Args& a, int at, Block4& x) {
+  int first = 0;
+  x.s = 0;
+  if (a.c.S > 1)
+    locate_item(a.c.S, at, [&](int sq) {
+      int b0, b1, unused;
+      span_of(a, sq, b0, b1, unused);
+      b0 = max(b0, 0);
+      return b1 > b0 ? (b1 - 1) / kBlock4 - b0 / kBlock4 + 1 : 0;
+    }, x.s, first);
+  if (x.s < 0) return false;
+  span_const(a, x.s, x.j0, x.j1, x.src0, x.src1, x.row0);
+  x.blk = max(x.j0, 0) / kBlock4 + (at - first);
+  return x.j1 > max(x.j0, 0) && x.blk * kBlock4 < x.j1;  // of the only sequence: up to its last
+}
+
+// The least and greatest of 8 channels of K over a lane's rows, from the values
+// as quantised, as ordered 16-bit integers two at a time; a NaN is a flag.
+struct Bounds4 {
+  uint32_t lo[4], hi[4];
+  bool bad = false;
+  __device__ __forceinline__ Bounds4() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      lo[i] = 0x7f807f80u;  // +inf, and -inf as it sorts
+      hi[i] = pk_sortable(0xff80ff80u);
+    }
+  }
+  __device__ __forceinline__ void add(uint32_t codes, uint32_t byte) {
+    if (byte == 255u) {
+      bad = true;
+      return;
+    }
+    const u32x4_t y = spread8(codes, scale_of(byte));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t t = pk_sortable(y[i]);
+      lo[i] = pk_min_i16(lo[i], t);
+      hi[i] = pk_max_i16(hi[i], t);
+    }
+  }
+};
+
+// The block's bounds from those of the workgroup's lanes, with the ones there are
+// where the block's first token is not the call's. red, bad_s: LDS.
+template <int D>
+__device__ __forceinline__ void store_bounds(const Cache4View& c, int lh, const Block4& x,
+                                             Bounds4 m,
+                                             uint32_t (&red)[kThreads / kWave][2][D / 2],
+                                             int (&bad_s)[kThreads / kWave][D / 8]) {
+  constexpr int PR = D / 8, NWV = kThreads / kWave;
+  const int tid = threadIdx.x, piece = tid % PR;
+  // over the rows of the wave (lanes of one piece), then over the waves
+#pragma unroll
+  for (int off = PR; off < kWave; off <<= 1) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      m.lo[i] = pk_min_i16(m.lo[i], (uint32_t)__shfl_xor((int)m.lo[i], off, kWave));
+      m.hi[i] = pk_max_i16(m.hi[i], (uint32_t)__shfl_xor((int)m.hi[i], off, kWave));
+    }
+  }
+  const uint64_t bads = ballot(m.bad);
+  if ((tid & 63) < PR) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      red[tid >> 6][0][4 * piece + i] = m.lo[i];
+      red[tid >> 6][1][4 * piece + i] = m.hi[i];
+    }
+    uint64_t lanes = 0;  // those that hold this piece
+#pragma unroll
+    for (int off = 0; off < kWave; off += PR) lanes |= uint64_t(1) << off;
+    bad_s[tid >> 6][piece] = (bads & (lanes << piece)) != 0;
+  }
+  __syncthreads();
+  uint16_t* __restrict__ bounds =
+      c.k_bounds + ((size_t)lh * c.nblk + x.row0 / kBlock4 + x.s + x.blk) * 2 * D;
+  if (tid < D) {
+    const int which = tid / (D / 2), two = tid % (D / 2);  // channels 2 two, 2 two + 1
+    uint32_t v = red[0][which][two];
+    bool nan0 = false, nan1;
+#pragma unroll
+    for (int w = 0; w < NWV; ++w) {
+      v = which ? pk_max_i16(v, red[w][which][two]) : pk_min_i16(v, red[w][which][two]);
+      nan0 |= bad_s[w][two / 4] != 0;
+    }
+    nan1 = nan0;
+    uint32_t* out = reinterpret_cast<uint32_t*>(bounds + which * D) + two;
+    if (x.blk * kBlock4 < x.j0) {  // the block's first token is not among the new ones
+      const uint32_t old = *out, t = pk_sortable(old);
+      nan0 |= (old & 0x7fffu) > 0x7f80u;
+      nan1 |= (old >> 16 & 0x7fffu) > 0x7f80u;
+      v = which ? pk_max_i16(v, t) : pk_min_i16(v, t);
+    }
+    v = pk_sortable(v);
+    if (nan0) v = (v & 0xffff0000u) | 0x7fc0u;
+    if (nan1) v = (v & 0xffffu) | 0x7fc00000u;
+    *out = v;
+  }
+}
+
 // One workgroup per (layer, KV head, block of 64 tokens): a lane holds 16
-// bytes (8 channels) of a row, a quad of lanes a group. The block's bounds of
-// K are taken from the values as quantised, as ordered 16-bit integers; a NaN
-// is a flag beside them. 32 layers x 8 heads x 1536 rows gathered from 32768 take
-// 51 us (255 MB, 5.0 TB/s), bound by the gather's reads in flight: 64 rows of K
-// and V a workgroup, 32 KB. Code stores are non-temporal (with ordinary ones 54
-// us; 16-byte stores of words exchanged within the quads 60).
+// bytes (8 channels) of a row, a quad of lanes a group. A token of the call
+// without a source keeps what its row holds, and the block's bounds count that
+// like the rows that are written. 32 layers x 8 heads x 1536 rows gathered from
+// 32768 take 51 us (255 MB, 5.0 TB/s), bound by the gather's reads in flight: 64
+// rows of K and V a workgroup, 32 KB. Code stores are non-temporal (with ordinary
+// ones 54 us; 16-byte stores of words exchanged within the quads 60).
 template <int D>
 __global__ __launch_bounds__(kThreads) void write4_kernel(Write4Args a) {
   constexpr int PR = D / 8;             // pieces of 8 channels a row
@@ -112,6 +219,8 @@ __global__ __launch_bounds__(kThreads) void write4_kernel(Write4Args a) {
   __shared__ int bad_s[NWV][PR];
   const int tid = threadIdx.x;
   const Cache4View& c = a.c;
+  // offsets of an append that count more tokens than it gives
+  const bool short_of = !a.cu_retained && read_const(a.cu_src, c.S) > a.nsrc;
   if (blockIdx.x == 0 && tid < kWave) {
     if (a.cu_retained) {
       bool over = false;
@@ -123,38 +232,32 @@ __global__ __launch_bounds__(kThreads) void write4_kernel(Write4Args a) {
       if (over && c.status) atomicOr(c.status, kFlagOutRows4);
     } else {
       report_rooms(c);
+      report_flags(c.status, short_of ? kFlagOutRows4 : 0u);
     }
   }
   if (a.nblocks == 0) return;
-  const int lh = uniform(blockIdx.x / a.nblocks), at = uniform(blockIdx.x - lh * a.nblocks);
+  const int lh = uniform(blockIdx.x / a.nblocks);
+  int at = uniform(blockIdx.x - lh * a.nblocks);
   const int l = uniform(lh / c.H), h = lh - l * c.H;
-  int s = 0, first = 0, j0, j1, src0, src1, row0;
-  if (c.S > 1)
-    locate_item(c.S, at, [&](int sq) {
-      int b0, b1, unused;
-      span_of(a, sq, b0, b1, unused);
-      b0 = max(b0, 0);
-      return b1 > b0 ? (b1 - 1) / kBlock4 - b0 / kBlock4 + 1 : 0;
-    }, s, first);
-  if (s < 0) return;  // past the last block: uniform over the workgroup
-  span_const(a, s, j0, j1, src0, src1, row0);
-  const int blk = max(j0, 0) / kBlock4 + (at - first);
-  if (j1 <= max(j0, 0) || blk * kBlock4 >= j1) return;  // past the only sequence's last block
+  Block4 x;
+  if (!find_block(a, at, x)) return;  // uniform over the workgroup
   const int32_t* __restrict__ idx =
-      a.idx ? a.idx + (a.shared_idx ? 0 : (size_t)lh * a.nsrc) + src0 : nullptr;
+      a.idx ? a.idx + (a.shared_idx ? 0 : (size_t)lh * a.nsrc) + x.src0 : nullptr;
   const int sub = tid / PR, piece = tid % PR;
-  int src[NP];  // source row, or -1
+  int src[NP];      // source row, or -1
+  int missing = 0;  // bit p: a token of the call that has none
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
-    const int j = blk * kBlock4 + p * RP + sub;
+    const int j = x.blk * kBlock4 + p * RP + sub;
     src[p] = -1;
-    if (j >= j0 && j < j1) {
+    if (j >= x.j0 && j < x.j1) {
       if (idx) {
         const int pos = idx[j];
-        if (pos >= 0 && pos < src1 - src0) src[p] = src0 + pos;
-      } else if (src0 + (j - j0) >= 0 && src0 + (j - j0) < a.nsrc) {
-        src[p] = src0 + (j - j0);
+        if (pos >= 0 && pos < x.src1 - x.src0) src[p] = x.src0 + pos;
+      } else if (x.src0 + (j - x.j0) >= 0 && x.src0 + (j - x.j0) < a.nsrc) {
+        src[p] = x.src0 + (j - x.j0);
       }
+      if (src[p] < 0) missing |= 1 << p;
     }
   }
   const uint16_t* __restrict__ kb = a.k + l * a.k_layer + h * a.k_head + 8 * piece;
@@ -167,15 +270,10 @@ __global__ __launch_bounds__(kThreads) void write4_kernel(Write4Args a) {
     kx[p] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(kb + src[p] * a.k_row));
     vx[p] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(vb + src[p] * a.v_row));
   }
-  const size_t first_row = (size_t)lh * c.rows + row0 + (size_t)blk * kBlock4;
-  uint32_t lo[4], hi[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    lo[i] = 0x7f807f80u;  // +inf, and -inf as it sorts
-    hi[i] = pk_sortable(0xff80ff80u);
-  }
-  uint32_t flags = 0;
-  bool bad = false;  // a NaN among this lane's channels of K
+  const size_t head_row = (size_t)lh * c.rows;
+  const size_t first_row = head_row + x.row0 + (size_t)x.blk * kBlock4;
+  Bounds4 m;
+  uint32_t flags = missing ? kFlagOutRows4 : 0u;
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
     uint32_t kbyte, vbyte;  // every lane: the quad exchanges need all four
@@ -189,65 +287,32 @@ __global__ __launch_bounds__(kThreads) void write4_kernel(Write4Args a) {
       c.k_scales[row * NS + piece / 4] = (uint8_t)kbyte;
       c.v_scales[row * NS + piece / 4] = (uint8_t)vbyte;
     }
-    if (kbyte == 255u) {
-      bad = true;
-    } else {
-      const u32x4_t y = spread8(kw, scale_of(kbyte));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t t = pk_sortable(y[i]);
-        lo[i] = pk_min_i16(lo[i], t);
-        hi[i] = pk_max_i16(hi[i], t);
-      }
-    }
+    m.add(kw, kbyte);
   }
   report_flags(c.status, flags);
   if (!c.k_bounds) return;
-  // over the rows of the wave (lanes of one piece), then over the waves
-#pragma unroll
-  for (int off = PR; off < kWave; off <<= 1) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      lo[i] = pk_min_i16(lo[i], (uint32_t)__shfl_xor((int)lo[i], off, kWave));
-      hi[i] = pk_max_i16(hi[i], (uint32_t)__shfl_xor((int)hi[i], off, kWave));
-    }
+  auto add_stored = [&](size_t row) __attribute__((always_inline)) {
+    m.add(reinterpret_cast<const uint32_t*>(c.k_codes + row * (D / 2))[piece],
+          c.k_scales[row * NS + piece / 4]);
+  };
+  if (ballot(missing != 0)) {  // rare
+#pragma nounroll
+    for (int p = 0; p < NP; ++p)
+      if (missing >> p & 1) add_stored(first_row + p * RP + sub);
   }
-  const uint64_t bads = ballot(bad);
-  if ((tid & 63) < PR) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      red[tid >> 6][0][4 * piece + i] = lo[i];
-      red[tid >> 6][1][4 * piece + i] = hi[i];
+  store_bounds<D>(c, lh, x, m, red, bad_s);
+  // Then the grid has fewer workgroups than there are blocks: those past it hold
+  // no token that is given (these come first), and only need their bounds.
+  if (!short_of) return;
+  for (at += a.nblocks; find_block(a, at, x); at += a.nblocks) {
+    __syncthreads();  // red and bad_s are read above
+    m = Bounds4();
+#pragma nounroll
+    for (int p = 0; p < NP; ++p) {
+      const int j = x.blk * kBlock4 + p * RP + sub;
+      if (j >= x.j0 && j < x.j1) add_stored(head_row + x.row0 + j);
     }
-    uint64_t lanes = 0;  // those that hold this piece
-#pragma unroll
-    for (int off = 0; off < kWave; off += PR) lanes |= uint64_t(1) << off;
-    bad_s[tid >> 6][piece] = (bads & (lanes << piece)) != 0;
-  }
-  __syncthreads();
-  uint16_t* __restrict__ bounds =
-      c.k_bounds + ((size_t)lh * c.nblk + row0 / kBlock4 + s + blk) * 2 * D;
-  if (tid < D) {
-    const int which = tid / (D / 2), two = tid % (D / 2);  // channels 2 two, 2 two + 1
-    uint32_t x = red[0][which][two];
-    bool nan0 = false, nan1;
-#pragma unroll
-    for (int w = 0; w < NWV; ++w) {
-      x = which ? pk_max_i16(x, red[w][which][two]) : pk_min_i16(x, red[w][which][two]);
-      nan0 |= bad_s[w][two / 4] != 0;
-    }
-    nan1 = nan0;
-    uint32_t* out = reinterpret_cast<uint32_t*>(bounds + which * D) + two;
-    if (blk * kBlock4 < j0) {  // the block's first token is not among the new ones
-      const uint32_t old = *out, t = pk_sortable(old);
-      nan0 |= (old & 0x7fffu) > 0x7f80u;
-      nan1 |= (old >> 16 & 0x7fffu) > 0x7f80u;
-      x = which ? pk_max_i16(x, t) : pk_min_i16(x, t);
-    }
-    x = pk_sortable(x);
-    if (nan0) x = (x & 0xffff0000u) | 0x7fc0u;
-    if (nan1) x = (x & 0xffffu) | 0x7fc00000u;
-    *out = x;
+    store_bounds<D>(c, lh, x, m, red, bad_s);
   }
 }
 

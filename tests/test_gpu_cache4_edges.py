@@ -1,0 +1,117 @@
+"""The 4-bit cache on the GPU where a call's arguments leave something out: rows without a source,
+and the block bounds over them. Everything is compared bit for bit with the fp64 oracle: every step
+of the format is exact, and so are least and greatest values."""
+import zlib
+
+import numpy as np
+import pytest
+
+import oracle.cache4_ref as R
+from oracle import decode_bf16
+from paper_2609_22158_amd import binding as B
+from paper_2609_22158_amd import cache4 as C4
+from tests.gpu_cases import log
+from tests.test_gpu_cache4 import bf16, host
+
+pytestmark = pytest.mark.gpu
+
+
+def full_cache(rng, L, H, d, rooms, nan_rows=()):
+    """A cache whose every row holds a token (some with a NaN key), and the values of its keys."""
+    import torch
+
+    n = sum(rooms)
+    cu = np.concatenate([[0], np.cumsum(rooms)]).astype(np.int32)
+    cache = C4.Cache4(L, H, d, cu)
+    k = bf16(rng, (L, n, H, d), 4.0)
+    for r in nan_rows:
+        k[:, r, :, 1] = 0x7FC0
+    dev = torch.from_numpy(cu).cuda()
+    C4.advance4(cache, dev)
+    C4.append4(cache, B.bf16_from_bits(k), B.bf16_from_bits(bf16(rng, (L, n, H, d))), dev)
+    cache.status(clear=True)
+    return cache, cu, stored_keys(cache)
+
+
+def stored_keys(cache):
+    codes, scales = host(cache)[:2]
+    return R.dequantise4(codes, scales)
+
+
+def check_all_bounds(cache, cu, lens):
+    """Every block's bounds are the least and greatest keys of the rows that hold its tokens."""
+    keys, got = stored_keys(cache), cache.k_bounds.float().cpu().numpy()
+    for s, n in enumerate(lens):
+        at, r = int(cu[s]) // 64 + s, int(cu[s])
+        for l in range(cache.num_layers):
+            for h in range(cache.num_kv_heads):
+                want = R.block_bounds(keys[l, h, r:r + n])
+                assert np.array_equal(got[l, h, at:at + len(want)], want, equal_nan=True), (l, h, s)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("shared", [False, True])
+def test_bounds_over_rows_that_a_compaction_leaves(d, shared, gpu_lib):
+    """Positions outside their sequence: single ones, a whole block of them (the bounds are those of
+    what its rows hold), one at a row with a NaN key, and a sequence of nothing else."""
+    import torch
+
+    log(f"[edges compact d={d} shared={shared}]")
+    rng = np.random.default_rng(zlib.crc32(b"left") + d)
+    L, H, src, kept, rooms = 2, 2, [700, 130, 40], [300, 65, 3], [310, 65, 64]
+    cache, cu, old = full_cache(rng, L, H, d, rooms, nan_rows=(200, 310 + 64))
+    cu_seq, cu_ret = (np.concatenate([[0], np.cumsum(x)]).astype(np.int32) for x in (src, kept))
+    n = int(cu_seq[-1])
+    k, v = bf16(rng, (L, H, n, d)), bf16(rng, (L, H, n, d))
+    idx = np.full((1 if shared else L * H, n), -7, np.int32)
+    bad = [(0, j) for j in [5, 200, 299] + list(range(64, 128))] + [(1, 64), (2, 0), (2, 1), (2, 2)]
+    for r in range(idx.shape[0]):
+        for s in range(3):
+            idx[r, cu_seq[s]:cu_seq[s] + kept[s]] = np.sort(rng.permutation(src[s])[:kept[s]])
+        for i, (s, j) in enumerate(bad):
+            idx[r, cu_seq[s] + j] = (-1, src[s], 1 << 30)[(i + r) % 3]
+    pb = B.Problem(L, H, H, d, 1, cu_seq, np.zeros(4, np.int32))
+    C4.compact4(pb, cache, B.bf16_from_bits(k), B.bf16_from_bits(v),
+                torch.from_numpy(idx[0] if shared else idx.reshape(L, H, n)).cuda(),
+                torch.from_numpy(cu_ret).cuda())
+    assert cache.lens.tolist() == kept
+    now = stored_keys(cache)
+    for s, j in bad:
+        assert np.array_equal(now[:, :, cu[s] + j], old[:, :, cu[s] + j], equal_nan=True)
+    check_all_bounds(cache, cu, kept)
+    assert cache.status() == B.FLAG_OUT_ROWS
+
+
+@pytest.mark.parametrize("num_new,counts", [(8, (6, 6, 0)), (1, (5, 500, 260)), (300, (300, 1, 129)),
+                                            (70, (0, 69, 3))])
+def test_bounds_over_rows_of_tokens_that_were_not_given(num_new, counts, gpu_lib):
+    """New tokens at or past num_new: their rows stay as they were, and every block that counts them
+    has bounds over what it holds, however many blocks they are."""
+    import torch
+
+    log(f"[edges append num_new={num_new} counts={counts}]")
+    rng = np.random.default_rng(zlib.crc32(b"given") + num_new)
+    L, H, d, rooms = 2, 1, 64, [400, 700, 261]
+    cache, cu, old = full_cache(rng, L, H, d, rooms, nan_rows=(390, 400 + 650))
+    cache.k_bounds.fill_(77.0)  # of nothing that the cache holds
+    before = [100, 3, 0]
+    first = torch.tensor(np.concatenate([[0], np.cumsum(before)]), dtype=torch.int32, device="cuda")
+    x = bf16(rng, (L, 103, H, d))
+    cache.lens.copy_(torch.tensor(before))
+    C4.append4(cache, B.bf16_from_bits(x), B.bf16_from_bits(x), first)
+    cu_new = torch.tensor(np.concatenate([[0], np.cumsum(counts)]), dtype=torch.int32, device="cuda")
+    y = bf16(rng, (L, num_new, H, d))
+    C4.advance4(cache, cu_new)
+    C4.append4(cache, B.bf16_from_bits(y), B.bf16_from_bits(y), cu_new)
+    lens = [a + b for a, b in zip(before, counts)]
+    assert cache.lens.tolist() == lens
+    now, at = stored_keys(cache), 0
+    for s, n in enumerate(counts):
+        r = cu[s] + before[s]
+        got = max(0, min(n, num_new - at))  # of the sequence's new tokens, those that were given
+        want = R.dequantise4(*R.quantise4(decode_bf16(y[:, at:at + got, 0])))
+        assert np.array_equal(now[:, 0, r:r + got], want)
+        assert np.array_equal(now[:, 0, r + got:cu[s + 1]], old[:, 0, r + got:cu[s + 1]], equal_nan=True)
+        at += n
+    check_all_bounds(cache, cu, lens)
+    assert cache.status() == (B.FLAG_OUT_ROWS if sum(counts) > num_new else 0)
