@@ -88,7 +88,8 @@ typedef struct stepkv_cache4 {
 /* eq. problem into 4 bits: for every (l, h) and sequence s, token
  * j < R_s = cu_retained[s+1] - cu_retained[s] of the cache becomes
  * k[l][h][cu_seqlens[s] + idx[l][h][cu_seqlens[s] + j]], and likewise v;
- * lens[s] = R_s. pb gives the source (num_layers, num_kv_heads, head_dim and
+ * lens[s] = R_s. (An R_s past the sequence's source tokens counts as these, and
+ * sets STEPKV_FLAG_OUT_ROWS.) pb gives the source (num_layers, num_kv_heads, head_dim and
  * num_seqs as the cache's); k, v, idx and cu_retained are as stepkv_compact's,
  * and idx is int32 [Ntot], one set for every layer and head, if shared_idx is
  * nonzero. A position outside its sequence leaves its row as it was

@@ -226,8 +226,9 @@ __global__ __launch_bounds__(kThreads) void write4_kernel(Write4Args a) {
       bool over = false;
       for (int s = tid; s < c.S; s += kWave) {
         const int n = max(a.cu_retained[s + 1] - a.cu_retained[s], 0);
-        c.lens[s] = n;
-        over |= n > c.cu_rows[s + 1] - c.cu_rows[s];
+        const int there = a.cu_src[s + 1] - a.cu_src[s];  // no more tokens than the source has
+        c.lens[s] = min(n, there);
+        over |= n > min(there, c.cu_rows[s + 1] - c.cu_rows[s]);
       }
       if (over && c.status) atomicOr(c.status, kFlagOutRows4);
     } else {

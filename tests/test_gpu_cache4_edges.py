@@ -115,3 +115,29 @@ def test_bounds_over_rows_of_tokens_that_were_not_given(num_new, counts, gpu_lib
         at += n
     check_all_bounds(cache, cu, lens)
     assert cache.status() == (B.FLAG_OUT_ROWS if sum(counts) > num_new else 0)
+
+
+def test_more_retained_rows_than_the_source_has(gpu_lib):
+    """A sequence gets no more tokens than its source has, whatever cu_retained counts, and that is
+    reported: the rows behind them, which nothing wrote, are not attended to."""
+    import torch
+
+    rng = np.random.default_rng(zlib.crc32(b"retained"))
+    L, H, d, src, rooms = 1, 2, 64, [40, 0, 90], [130, 20, 100]
+    cache, cu, old = full_cache(rng, L, H, d, rooms, nan_rows=(45, 135, 245))
+    cu_seq = np.concatenate([[0], np.cumsum(src)]).astype(np.int32)
+    n = int(cu_seq[-1])
+    k, v = bf16(rng, (L, H, n, d)), bf16(rng, (L, H, n, d))
+    idx = np.concatenate([np.arange(x) for x in src]).astype(np.int32)
+    pb = B.Problem(L, H, H, d, 1, cu_seq, np.zeros(4, np.int32))
+    C4.compact4(pb, cache, B.bf16_from_bits(k), B.bf16_from_bits(v), torch.from_numpy(idx).cuda(),
+                torch.tensor([0, 50, 57, 157], dtype=torch.int32, device="cuda"))
+    assert cache.lens.tolist() == src
+    assert cache.status(clear=True) == B.FLAG_OUT_ROWS
+    check_all_bounds(cache, cu, src)
+    now = stored_keys(cache)
+    for s, m in enumerate(src):
+        assert np.array_equal(now[:, :, cu[s] + m:cu[s + 1]], old[:, :, cu[s] + m:cu[s + 1]], equal_nan=True)
+    q = torch.ones((L, 3, H, d), dtype=torch.bfloat16, device="cuda")
+    out = C4.decode_attention4(cache, q)
+    assert torch.isfinite(out).all() and (out[0, 1] == 0).all() and cache.status() == 0
