@@ -171,9 +171,10 @@ size_t stepkv_cache4_select_workspace_bytes(const stepkv_cache4* c);
  * and those others with the greatest score
  *   score(b) = sum over the heads g of the KV head and the channels i of
  *              max(q_gi kmin_bi, q_gi kmax_bi),
- * an upper bound of the group's summed logits in the block, computed in 64
- * bits; a NaN score ranks as -inf, equal scores the lower block first. Written
- * ascending to blocks int32 [L][S][H][num_blocks], -1 past the last; all the
+ * (q kmax where q > 0, q kmin where q < 0), an upper bound of the group's summed
+ * logits in the block, computed in 64 bits; a NaN score ranks as -inf, equal
+ * scores the lower block first. So a NaN in any of the group's queries, which
+ * makes every score NaN, lists the lowest blocks. Written ascending to blocks int32 [L][S][H][num_blocks], -1 past the last; all the
  * blocks of a sequence that has no more than num_blocks.
  * Errors: EINVAL (also a cache without k_bounds, num_blocks < 1, negative
  * counts, first_blocks + last_blocks > num_blocks), EUNSUPPORTED (d, rows),

@@ -103,7 +103,7 @@ __device__ __forceinline__ void score_blocks(const uint16_t* __restrict__ q, int
 #pragma unroll 8
     for (int g = 0; g < G; ++g) {
       const float y = bf16_float(q[(size_t)g * D + threadIdx.x]);
-      up += y > 0.f ? (double)y : 0.0;  // a NaN adds nothing
+      up += !(y <= 0.f) ? (double)y : 0.0;  // a NaN too: it makes every score one
       down += y < 0.f ? (double)y : 0.0;
     }
     coef[0][threadIdx.x] = down;  // of the minimum

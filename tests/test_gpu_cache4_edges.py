@@ -141,3 +141,31 @@ def test_more_retained_rows_than_the_source_has(gpu_lib):
     q = torch.ones((L, 3, H, d), dtype=torch.bfloat16, device="cuda")
     out = C4.decode_attention4(cache, q)
     assert torch.isfinite(out).all() and (out[0, 1] == 0).all() and cache.status() == 0
+
+
+@pytest.mark.parametrize("lens,n", [([64 * 40], 5), ([64 * 900, 3000], 7), ([64 * 5000], 100)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_nan_in_one_query_of_a_group(d, lens, n, gpu_lib):
+    """One NaN element of one head makes every score of its group NaN, which ranks as -inf: the lowest
+    blocks beside the forced ones. Other groups, sequences and layers rank theirs as before."""
+    import torch
+
+    L, H, G, S = 2, 2, 3, len(lens)
+    cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(12)
+    x = torch.randn((L, H, int(cu[-1]) // 64 + S, 2, d), generator=gen, device="cuda")
+    bounds = x.sort(dim=3).values.bfloat16()
+    cache = C4.Cache4(L, H, d, cu, k_bounds=bounds, lens=torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    q = torch.randn((L, S, H * G, d), generator=gen, device="cuda").bfloat16()
+    q[1, 0, 4, 17] = float("nan")
+    got = C4.select_blocks4(cache, q, n, first=1, last=2).cpu().numpy()
+    for s in range(S):
+        nb, at = -(-lens[s] // 64), int(cu[s]) // 64 + s
+        for l in range(L):
+            for h in range(H):
+                score = R.block_scores(q[l, s, h * G:(h + 1) * G].double().cpu().numpy(),
+                                       bounds[l, h, at:at + nb].double().cpu().numpy())
+                assert np.isnan(score).all() == ((l, s, h) == (1, 0, 1))
+                assert np.array_equal(got[l, s, h], R.select_blocks(score, n, 1, 2)), (l, s, h)
+    assert got[1, 0, 1].tolist() == list(range(n - 2)) + [-(-lens[0] // 64) - 2, -(-lens[0] // 64) - 1]
