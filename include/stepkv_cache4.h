@@ -147,7 +147,8 @@ size_t stepkv_cache4_decode_workspace_bytes(const stepkv_cache4* c, int32_t num_
  * out fp32 [L][S][Hq][d]; lse fp32 [L][S][Hq] or NULL: the natural-log
  * log-sum-exp of the row's logits, with which results over several caches can
  * be joined. A sequence without tokens gives zeros, and -inf. scale <= 0
- * selects 1/sqrt(d).
+ * selects 1/sqrt(d). A logit that overflows fp32 to -inf has no weight; where
+ * every one does, the result is NaN, and the log-sum-exp -inf.
  * blocks (int32 [L][S][H][num_blocks], or NULL with num_blocks 0): attention
  * over the tokens of the listed blocks only, an ascending list per (layer,
  * sequence, KV head); an entry that is no block of the sequence (-1), or is

@@ -147,10 +147,16 @@ __device__ __forceinline__ Parts<C> split_parts(const float (&p)[8], int copy) {
   return r;
 }
 
+// The reference of a wave that saw tokens, whose logits are all -inf: below every
+// logit, but not that of a wave without tokens.
+constexpr float kNoWeight = -3.40282347e38f;
+
 // The result of a query head from its sums (row: (layer, sequence, query head)).
+// Without a token zeros; where every logit is -inf (an overflow) the softmax of
+// such logits, 0 / 0.
 __device__ __forceinline__ void finish(const Attend4Args& a, size_t row, int ch, int D, float M,
                                        float Z, float O) {
-  a.out[row * D + ch] = Z == 0.f ? 0.f : O / Z;  // no token: zeros
+  a.out[row * D + ch] = M == -INFINITY && Z == 0.f ? 0.f : O / Z;
   if (a.lse && ch == 0) a.lse[row] = Z == 0.f ? -INFINITY : (M + log2f(Z)) * 0.693147180559945309f;
 }
 
@@ -393,6 +399,7 @@ void attend4_kernel(Attend4Args a) {
               __builtin_amdgcn_mfma_f32_16x16x32_bf16(pp.x[k], vb[i], o[nb0 + i], 0, 0, 0);
     }
   };
+  bool any = false;  // a tile with tokens
   if (t0 < t1) {
     Tile cur;
     load(cur, t0);
@@ -402,6 +409,7 @@ void attend4_kernel(Attend4Args a) {
       if (some) consume(cur);
       load(cur, t + 1);
       if (some) attend(tok);
+      any |= some;
     }
   }
   __syncthreads();  // the states overwrite the V tiles of every wave
@@ -418,7 +426,8 @@ void attend4_kernel(Attend4Args a) {
       if (c16 == 0) state[wave][4 * g4 + i][D + 1] = z[i];
     }
   }
-  if (g4 == 0 && c16 < heads) state[wave][c16][D] = m_ref;  // the same in every copy
+  if (g4 == 0 && c16 < heads)  // the same in every copy
+    state[wave][c16][D] = any ? fmaxf(m_ref, kNoWeight) : -INFINITY;
   __syncthreads();
   float* const part = a.partial + ((size_t)unit * a.splits + gs) * min(a.G, 16) * ST;
   const size_t row_out = ((size_t)l * c.S + s) * a.Hq + h * a.G + hd0;

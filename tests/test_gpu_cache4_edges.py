@@ -169,3 +169,70 @@ def test_a_nan_in_one_query_of_a_group(d, lens, n, gpu_lib):
                 assert np.isnan(score).all() == ((l, s, h) == (1, 0, 1))
                 assert np.array_equal(got[l, s, h], R.select_blocks(score, n, 1, 2)), (l, s, h)
     assert got[1, 0, 1].tolist() == list(range(n - 2)) + [-(-lens[0] // 64) - 2, -(-lens[0] // 64) - 1]
+
+
+LOST = {
+    # name: (G, d, tokens of each sequence, which tokens have a logit of -inf)
+    "one_split": (3, 64, [500, 64, 0, 33], lambda s, j: s != 3 or j < 20),
+    "one_split_g7": (7, 128, [700, 65, 1], lambda s, j: s == 0 or j < 32),
+    "splits": (3, 128, [6000, 2000, 0], lambda s, j: s == 0 or j < 1700),
+    "splits_g7": (7, 64, [9000, 4000], lambda s, j: s == 0 or (j // 128) % 2 == 0),
+    "many": (1, 64, [2100 if i % 40 == 0 else 70 for i in range(600)], lambda s, j: s % 2 == 0 or j < 64),
+}
+
+
+@pytest.mark.parametrize("cid", list(LOST))
+def test_logits_of_minus_infinity(cid, gpu_lib):
+    """Head 0's logits are 0, or overflow to -inf. A token of -inf has no weight beside others; where
+    there is no other, the result is the softmax of such logits, NaN (not the zeros of a sequence
+    without tokens), and the log-sum-exp -inf. Over lists of blocks alike. A mean over n values in
+    fp32: off by (2 n + 64) u of the mean magnitude, as the other sums of attention's tests."""
+    import torch
+
+    from tests.test_gpu_attend4 import Made, U
+
+    G, d, lens, gone = LOST[cid]
+    log(f"[edges -inf {cid}] tokens={lens[:4]}")
+    m = Made("lost " + cid, 1, G, 1, d, lens, [n + 3 for n in lens])
+    S = len(lens)
+    away = [np.array([gone(s, j) for j in range(n)], bool) for s, n in enumerate(lens)]
+    for s in range(S):
+        a = m.cu[s]
+        m.k_bits[0, a:a + lens[s], 0, 0] = np.where(away[s], 0xC100, 0)  # -8, exact in 4 bits here
+    m.q_bits[0, :, 0] = 0
+    m.q_bits[0, :, 0, 0] = 0x7F60  # 2.98e38: times -8 past fp32's range
+    m.write()
+    assert all((m.rows(0, s, 0)[0][:, 0] == np.where(away[s], -8, 0)).all() for s in range(S))
+
+    def check(out, lse, seen):
+        out, lse = out.cpu().numpy()[0, :, 0], lse.cpu().numpy()[0, :, 0]
+        for s, n in enumerate(lens):
+            keep = seen[s] & ~away[s]
+            if not seen[s].any():
+                assert (out[s] == 0).all() and lse[s] == -np.inf, s
+            elif not keep.any():
+                assert np.isnan(out[s]).all() and lse[s] == -np.inf, s
+            else:
+                v = m.rows(0, s, 0)[1][keep]
+                steps = 2.0 ** -19 + (2 * n + 64) * U
+                assert (np.abs(out[s] - v.mean(axis=0)) <= 2 * steps * np.abs(v).mean(axis=0)).all(), s
+                assert abs(lse[s] - np.log(len(v))) <= steps + 4 * U * np.log(len(v)), s
+
+    out, lse = C4.decode_attention4(m.cache, m.q, want_lse=True)
+    check(out, lse, [np.ones(n, bool) for n in lens])
+    assert torch.isfinite(out[:, :, 1:]).all()
+    rng = np.random.default_rng(3)
+    most = max(-(-n // 64) for n in lens)
+    for n in (2, most):
+        lists = np.full((1, S, 1, n), -1, np.int32)
+        seen = []
+        for s in range(S):
+            nb = -(-lens[s] // 64)
+            pick = np.sort(rng.permutation(nb)[:rng.integers(0, min(n, nb) + 1)])
+            lists[0, s, 0, :len(pick)] = pick
+            keep = np.zeros(nb, bool)
+            keep[pick] = True
+            seen.append(keep.repeat(64)[:lens[s]])
+        out, lse = C4.decode_attention4(m.cache, m.q, blocks=torch.from_numpy(lists).cuda(), want_lse=True)
+        check(out, lse, seen)
+    assert m.cache.status() == 0
