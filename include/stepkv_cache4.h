@@ -60,8 +60,11 @@ extern "C" {
 
 #define STEPKV_CACHE4_BLOCK 64 /* tokens of a block */
 #define STEPKV_CACHE4_GROUP 32 /* channels of a scale */
-/* Rows of a (layer, KV head), cu_rows[S] (EUNSUPPORTED beyond): sums of rows and
- * of a split's length stay within 31 bits. */
+/* Rows of a (layer, KV head), cu_rows[S], and of a read (EUNSUPPORTED beyond):
+ * sums of rows and of a split's length stay within 31 bits. A call whose launch
+ * would have 2^32 threads or more (2^24 workgroups of 256: as many blocks of 64
+ * rows written, or sequences attended to, over all layers and heads) is
+ * EUNSUPPORTED too. */
 #define STEPKV_CACHE4_MAX_ROWS ((1 << 30) - (1 << 20))
 
 /* A cache: its shape, the rows of its sequences, and its device buffers (all
@@ -130,7 +133,7 @@ int stepkv_cache4_append(const stepkv_cache4* c, const void* k_new, const int64_
  * sequences, in the layout that stepkv_score takes. Rows at or past out_rows
  * and rows without a token are left as they were. k_out or v_out may be NULL:
  * it is not read back. Errors: EINVAL (both NULL with out_rows > 0, negative
- * out_rows, misaligned pointers), EUNSUPPORTED (d, rows), EHIP. */
+ * out_rows, misaligned pointers), EUNSUPPORTED (d, rows, out_rows), EHIP. */
 int stepkv_cache4_read(const stepkv_cache4* c, const int32_t* cu_out, int32_t out_rows,
                        void* k_out, void* v_out, void* stream);
 

@@ -43,6 +43,7 @@ typedef short i16x4_t __attribute__((__vector_size__(4 * sizeof(short))));
 
 constexpr int kTile = 32;  // tokens a wave computes at a time
 constexpr int kWaves = 4;  // waves of a workgroup
+constexpr int kMergeThreads = 256;  // of a merge of many rows
 constexpr float kSlack = 16.f;
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -594,6 +595,13 @@ size_t attend4_partial_floats(const Attend4Args& a) {
   return (size_t)a.c.L * a.c.H * ((a.G + 15) / 16) * a.splits * std::min(a.G, 16) * (a.c.d + 2);
 }
 
+bool attend4_fits(const Attend4Args& a) {
+  const int64_t units = (int64_t)a.c.L * a.c.H * ((a.G + 15) / 16);
+  // 8 waves a workgroup only where there are few; the merge's where there are many
+  return grid_fits((units * a.splits + 7) / 8 * 8, kWaves * kWave) &&
+         (a.single || grid_fits(units * a.c.S, kMergeThreads));
+}
+
 namespace {
 
 template <int D>
@@ -616,7 +624,8 @@ void launch_attend(const Attend4Args& a, hipStream_t st) {
   if (a.single) return;
   const unsigned rows = units * (unsigned)a.c.S;
   if (rows >= 512)
-    hipLaunchKernelGGL((combine4_kernel<D, 256, false>), dim3(rows), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((combine4_kernel<D, kMergeThreads, false>), dim3(rows), dim3(kMergeThreads),
+                       0, st, a);
   else
     hipLaunchKernelGGL((combine4_kernel<D, 512, true>), dim3(rows * std::min(a.G, 16)), dim3(512),
                        0, st, a);

@@ -317,21 +317,35 @@ void plan_select4(Select4Args& a, const int32_t* cu_rows_host) {
 
 namespace {
 
+// Threads of a workgroup of select4_kernel, and whether it holds few keys: with
+// many rows of short sequences more workgroups share a compute unit.
+bool few_keys(const Select4Args& a) {
+  return a.chunks == 0 && (int64_t)a.c.L * a.c.S * a.c.H >= 512 && a.most <= 1024;
+}
+int select_threads(const Select4Args& a) {
+  return a.chunks > 0 ? 512 : few_keys(a) ? kThreads : 1024;
+}
+
 template <int D>
 void launch_select(const Select4Args& a, hipStream_t st) {
-  const unsigned rows = (unsigned)(a.c.L * a.c.S) * (unsigned)a.c.H;
+  const dim3 rows((unsigned)(a.c.L * a.c.S) * (unsigned)a.c.H), threads(select_threads(a));
   if (a.chunks > 0) {
     hipLaunchKernelGGL(score4_kernel<D>, dim3((unsigned)(a.c.L * a.c.H) * (unsigned)a.chunks),
                        dim3(kThreads), 0, st, a);
-    hipLaunchKernelGGL((select4_kernel<D, 512, false, kLdsBlocks>), dim3(rows), dim3(512), 0, st, a);
-  } else if (rows >= 512 && a.most <= 1024) {
-    hipLaunchKernelGGL((select4_kernel<D, kThreads, true, 1024>), dim3(rows), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL((select4_kernel<D, 512, false, kLdsBlocks>), rows, threads, 0, st, a);
+  } else if (few_keys(a)) {
+    hipLaunchKernelGGL((select4_kernel<D, kThreads, true, 1024>), rows, threads, 0, st, a);
   } else {
-    hipLaunchKernelGGL((select4_kernel<D, 1024, true, kLdsBlocks>), dim3(rows), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL((select4_kernel<D, 1024, true, kLdsBlocks>), rows, threads, 0, st, a);
   }
 }
 
 }  // namespace
+
+bool select4_fits(const Select4Args& a) {
+  return grid_fits((int64_t)a.c.L * a.c.H * a.chunks, kThreads) &&
+         grid_fits((int64_t)a.c.L * a.c.S * a.c.H, select_threads(a));
+}
 
 hipError_t launch_select4(const Select4Args& a, hipStream_t st) {
   if (a.c.d == 128) launch_select<128>(a, st);

@@ -11,6 +11,12 @@ namespace stepkv {
 constexpr int kBlock4 = 64;  // tokens of a block (STEPKV_CACHE4_BLOCK)
 constexpr int kGroup4 = 32;  // channels of a scale (STEPKV_CACHE4_GROUP)
 
+// A launch has fewer than 2^32 threads: of more, it runs the first modulo 2^32 and
+// reports no error.
+inline bool grid_fits(int64_t workgroups, int threads) {
+  return workgroups <= (int64_t)UINT32_MAX / threads;
+}
+
 // The cache as the kernels see it.
 struct Cache4View {
   uint8_t* k_codes;          // [L*H][rows][d/2]
@@ -37,6 +43,7 @@ struct Write4Args {
   int shared_idx;
   int nblocks;               // (sequence, block) pairs a (layer, head) can touch
 };
+bool write4_fits(const Write4Args& a);
 hipError_t launch_write4(const Write4Args& a, hipStream_t st);
 hipError_t launch_advance4(const Cache4View& c, const int32_t* cu_new, hipStream_t st);
 
@@ -47,6 +54,7 @@ struct Read4Args {
   uint16_t* v_out;
   int out_rows;
 };
+bool read4_fits(const Read4Args& a);
 hipError_t launch_read4(const Read4Args& a, hipStream_t st);
 
 // ---------------------------------------------------------------- attention
@@ -66,6 +74,7 @@ struct Attend4Args {
 // Fills splits, min_rows and single from the shape and the rooms of the sequences.
 void plan_attend4(Attend4Args& a, const int32_t* cu_rows_host);
 size_t attend4_partial_floats(const Attend4Args& a);
+bool attend4_fits(const Attend4Args& a);
 hipError_t launch_attend4(const Attend4Args& a, hipStream_t st);
 
 // ---------------------------------------------------------------- block selection
@@ -80,6 +89,7 @@ struct Select4Args {
 };
 // Fills chunks and most from the shape and the rooms of the sequences.
 void plan_select4(Select4Args& a, const int32_t* cu_rows_host);
+bool select4_fits(const Select4Args& a);
 hipError_t launch_select4(const Select4Args& a, hipStream_t st);
 
 }  // namespace stepkv

@@ -407,6 +407,10 @@ __global__ __launch_bounds__(kThreads) void read4_kernel(Read4Args a) {
 
 }  // namespace
 
+bool write4_fits(const Write4Args& a) {
+  return grid_fits((int64_t)a.c.L * a.c.H * a.nblocks, kThreads);
+}
+
 hipError_t launch_write4(const Write4Args& a, hipStream_t st) {
   // one workgroup at least: the compaction sets lens
   const dim3 grid(a.nblocks > 0 ? (unsigned)(a.c.L * a.c.H) * (unsigned)a.nblocks : 1u);
@@ -422,23 +426,35 @@ hipError_t launch_advance4(const Cache4View& c, const int32_t* cu_new, hipStream
   return hipGetLastError();
 }
 
+namespace {
+
+// Workgroups of a read with `passes` rows a thread.
+int64_t read_workgroups(const Read4Args& a, int passes) {
+  const int64_t rows = (int64_t)kThreads / (a.c.d / 8) * passes;
+  return (int64_t)a.c.L * a.c.H * ((a.out_rows + rows - 1) / rows);
+}
+
+}  // namespace
+
+bool read4_fits(const Read4Args& a) { return grid_fits(read_workgroups(a, 4), kThreads); }
+
 hipError_t launch_read4(const Read4Args& a, hipStream_t st) {
   // One row per thread keeps the most workgroups in flight, and the smallest
   // calls short (32 layers x 8 heads x 1536 rows 42 us, with four rows 47; 85
   // rows 4.1 and 6.0). With many rows of several sequences the search for the
   // sequence counts: four rows share it (28 layers x 4 heads x 16 sequences,
-  // 28800 rows in all: 358 us, with one row 380).
-  const int rp = kThreads / (a.c.d / 8);
-  const int64_t one = (int64_t)a.c.L * a.c.H * ((a.out_rows + rp - 1) / rp);
+  // 28800 rows in all: 358 us, with one row 380). Four rows also keep the largest
+  // reads of one sequence within a launch (2^28 rows of d 128, all heads together).
+  const int64_t one = read_workgroups(a, 1);
   auto run = [&](auto passes) {
     constexpr int P = decltype(passes)::value;
-    const dim3 grid((unsigned)(a.c.L * a.c.H) * (unsigned)((a.out_rows + P * rp - 1) / (P * rp)));
+    const dim3 grid((unsigned)read_workgroups(a, P));
     if (a.c.d == 128)
       hipLaunchKernelGGL((read4_kernel<128, P>), grid, dim3(kThreads), 0, st, a);
     else
       hipLaunchKernelGGL((read4_kernel<64, P>), grid, dim3(kThreads), 0, st, a);
   };
-  if (a.c.S > 1 && one >= 8 * 2048) run(std::integral_constant<int, 4>{});
+  if ((a.c.S > 1 && one >= 8 * 2048) || !grid_fits(one, kThreads)) run(std::integral_constant<int, 4>{});
   else run(std::integral_constant<int, 1>{});
   return hipGetLastError();
 }

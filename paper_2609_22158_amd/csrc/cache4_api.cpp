@@ -74,9 +74,6 @@ Cache4View view(const stepkv_cache4* c) {
   return w;
 }
 
-// A launch has at most 2^31 - 1 workgroups.
-bool grid_fits(int64_t workgroups) { return workgroups <= std::numeric_limits<int32_t>::max() - 8; }
-
 Attend4Args attend_args(const stepkv_cache4* c, int32_t num_q_heads, int32_t num_blocks) {
   Attend4Args a{};
   a.c = view(c);
@@ -116,10 +113,6 @@ size_t partial_bytes(const Attend4Args& a) {
   return align_up(sizeof(float) * attend4_partial_floats(a));
 }
 
-bool attend_fits(const Attend4Args& a) {
-  return grid_fits((int64_t)a.c.L * a.c.H * ((a.G + 15) / 16) * a.splits);
-}
-
 int run_attend(const stepkv_cache4* c, Attend4Args a, const void* q_dec, const int32_t* blocks,
                float scale, float* out, float* lse, void* workspace, hipStream_t st) {
   a.q = static_cast<const uint16_t*>(q_dec);
@@ -131,9 +124,9 @@ int run_attend(const stepkv_cache4* c, Attend4Args a, const void* q_dec, const i
   return hip_status(launch_attend4(a, st));
 }
 
-int run_select(const stepkv_cache4* c, int32_t num_q_heads, const void* q_dec,
-               int32_t num_blocks, int32_t first_blocks, int32_t last_blocks, int32_t* blocks,
-               void* workspace, hipStream_t st) {
+Select4Args select_args(const stepkv_cache4* c, int32_t num_q_heads, const void* q_dec,
+                        int32_t num_blocks, int32_t first_blocks, int32_t last_blocks,
+                        int32_t* blocks, void* workspace) {
   Select4Args a;
   a.c = view(c);
   a.q = static_cast<const uint16_t*>(q_dec);
@@ -145,8 +138,7 @@ int run_select(const stepkv_cache4* c, int32_t num_q_heads, const void* q_dec,
   a.first = first_blocks;
   a.last = last_blocks;
   plan_select4(a, c->cu_rows_host);
-  if (!grid_fits((int64_t)c->num_layers * c->num_kv_heads * a.chunks)) return STEPKV_EUNSUPPORTED;
-  return hip_status(launch_select4(a, st));
+  return a;
 }
 
 }  // namespace
@@ -184,8 +176,7 @@ int stepkv_cache4_compact(const stepkv_problem* pb, const stepkv_cache4* c, cons
     nb += ((int64_t)std::min(room, n) + kBlock4 - 1) / kBlock4;
   }
   a.nblocks = (int)nb;
-  if (!grid_fits((int64_t)c->num_layers * c->num_kv_heads * std::max<int64_t>(nb, 1)))
-    return STEPKV_EUNSUPPORTED;
+  if (!write4_fits(a)) return STEPKV_EUNSUPPORTED;
   return hip_status(launch_write4(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -225,7 +216,7 @@ int stepkv_cache4_append(const stepkv_cache4* c, const void* k_new, const int64_
   a.shared_idx = 0;
   // n rows in order touch at most floor((n - 1) / 64) + 2 blocks, and at most n
   a.nblocks = (int)std::min<int64_t>(num_new, (int64_t)num_new / kBlock4 + 2 * (int64_t)c->num_seqs);
-  if (!grid_fits((int64_t)c->num_layers * c->num_kv_heads * a.nblocks)) return STEPKV_EUNSUPPORTED;
+  if (!write4_fits(a)) return STEPKV_EUNSUPPORTED;
   return hip_status(launch_write4(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -242,8 +233,7 @@ int stepkv_cache4_read(const stepkv_cache4* c, const int32_t* cu_out, int32_t ou
   a.k_out = static_cast<uint16_t*>(k_out);
   a.v_out = static_cast<uint16_t*>(v_out);
   a.out_rows = out_rows;
-  if (!grid_fits((int64_t)c->num_layers * c->num_kv_heads * ((int64_t)out_rows / 16 + 1)))
-    return STEPKV_EUNSUPPORTED;
+  if (out_rows > STEPKV_CACHE4_MAX_ROWS || !read4_fits(a)) return STEPKV_EUNSUPPORTED;
   return hip_status(launch_read4(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -262,7 +252,7 @@ int stepkv_cache4_decode(const stepkv_cache4* c, int32_t num_q_heads, const void
   if (rc != STEPKV_OK) return rc;
   if (blocks ? num_blocks < 1 : num_blocks != 0) return STEPKV_EINVAL;
   const Attend4Args a = attend_args(c, num_q_heads, num_blocks);
-  if (!attend_fits(a)) return STEPKV_EUNSUPPORTED;
+  if (!attend4_fits(a)) return STEPKV_EUNSUPPORTED;
   const size_t need = partial_bytes(a);
   if (need > 0 && (!workspace || !aligned(workspace, kAlign) || ws_bytes < need))
     return STEPKV_EWORKSPACE;
@@ -284,8 +274,10 @@ int stepkv_cache4_select_blocks(const stepkv_cache4* c, int32_t num_q_heads, con
   if (rc != STEPKV_OK) return rc;
   if (!workspace || !aligned(workspace, kAlign) || ws_bytes < keys_bytes(c))
     return STEPKV_EWORKSPACE;
-  return run_select(c, num_q_heads, q_dec, num_blocks, first_blocks, last_blocks, blocks,
-                    workspace, static_cast<hipStream_t>(stream));
+  const Select4Args a = select_args(c, num_q_heads, q_dec, num_blocks, first_blocks, last_blocks,
+                                    blocks, workspace);
+  if (!select4_fits(a)) return STEPKV_EUNSUPPORTED;
+  return hip_status(launch_select4(a, static_cast<hipStream_t>(stream)));
 }
 
 size_t stepkv_cache4_sparse_workspace_bytes(const stepkv_cache4* c, int32_t num_q_heads,
@@ -306,15 +298,18 @@ int stepkv_cache4_decode_sparse(const stepkv_cache4* c, int32_t num_q_heads, con
     rc = check_select(c, num_q_heads, q_dec, num_blocks, first_blocks, last_blocks, blocks);
   if (rc != STEPKV_OK) return rc;
   const Attend4Args a = attend_args(c, num_q_heads, num_blocks);
-  if (!attend_fits(a)) return STEPKV_EUNSUPPORTED;
+  if (!attend4_fits(a)) return STEPKV_EUNSUPPORTED;
+  const Select4Args b = select_args(c, num_q_heads, q_dec, num_blocks, first_blocks, last_blocks,
+                                    blocks, workspace);
+  if (!select4_fits(b)) return STEPKV_EUNSUPPORTED;
   const size_t keys = keys_bytes(c);
   if (!workspace || !aligned(workspace, kAlign) || ws_bytes < keys + partial_bytes(a))
     return STEPKV_EWORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  uint8_t* ws = static_cast<uint8_t*>(workspace);
-  rc = run_select(c, num_q_heads, q_dec, num_blocks, first_blocks, last_blocks, blocks, ws, st);
+  rc = hip_status(launch_select4(b, st));
   if (rc != STEPKV_OK) return rc;
-  return run_attend(c, a, q_dec, blocks, scale, out, lse, ws + keys, st);
+  return run_attend(c, a, q_dec, blocks, scale, out, lse, static_cast<uint8_t*>(workspace) + keys,
+                    st);
 }
 
 }  // extern "C"

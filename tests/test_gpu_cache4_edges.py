@@ -236,3 +236,23 @@ def test_logits_of_minus_infinity(cid, gpu_lib):
         out, lse = C4.decode_attention4(m.cache, m.q, blocks=torch.from_numpy(lists).cuda(), want_lse=True)
         check(out, lse, seen)
     assert m.cache.status() == 0
+
+
+def test_a_read_of_more_rows_than_one_row_a_thread_covers(gpu_lib):
+    """2^28 rows and some of d 128 (64 GiB): past a launch of one row a thread. The tokens are the
+    last rows; the others stay as they were."""
+    import torch
+
+    rows, n, d = 2 ** 28 + 1000, 100, 128
+    if torch.cuda.mem_get_info()[0] < (rows * d * 2) + (8 << 30):
+        pytest.skip("not enough memory on this GPU")
+    rng = np.random.default_rng(zlib.crc32(b"read"))
+    cache, cu, keys = full_cache(rng, 1, 1, d, [n])
+    out = torch.empty((1, 1, rows, d), dtype=torch.bfloat16, device="cuda")
+    tail = out[0, 0, -5000:]
+    tail.fill_(7.0)
+    C4.read4(cache, torch.tensor([0, rows], dtype=torch.int32, device="cuda"), rows, k_out=out, v_out=False)
+    got = tail.float().cpu().numpy()
+    del out, tail
+    torch.cuda.empty_cache()
+    assert (got[:-n] == 7).all() and np.array_equal(got[-n:], keys[0, 0])
