@@ -106,6 +106,8 @@ class Cache4:
         self.cu_rows.setflags(write=False)
         if self.cu_rows.ndim != 1 or self.cu_rows.size < 2:
             raise ValueError("cu_rows: the row offsets of one sequence or more")
+        if not np.array_equal(self.cu_rows, cu_rows):
+            raise ValueError("cu_rows: offsets that int32 does not hold")
         self.num_seqs = int(self.cu_rows.size - 1)
         self.rows = int(self.cu_rows[-1])
         self.device = _device(device)

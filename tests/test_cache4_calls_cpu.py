@@ -91,3 +91,11 @@ def test_refuses_more_than_a_launch_takes(call):
     rooms, fn = TOO_LARGE[call]
     c = _cache(*rooms) if isinstance(rooms[0], list) else _cache(rooms)
     assert fn(C4.load(), c) == B.EUNSUPPORTED
+
+
+# ---------------------------------------------------------------- values that would change silently
+@pytest.mark.parametrize("cu", [np.array([0, 2 ** 32 + 100]), np.array([0.0, 100.5]), [0, 2 ** 33],
+                                np.array([0, 10, -2 ** 32 + 64])])
+def test_refuses_row_offsets_that_int32_does_not_hold(cu):
+    with pytest.raises((ValueError, OverflowError)):
+        C4.Cache4(1, 1, 64, cu, device="cpu")
