@@ -161,8 +161,9 @@ size_t stepkv_cache4_decode_workspace_bytes(const stepkv_cache4* c, int32_t num_
  * exact products, the probabilities in fp32. Results are
  * the same from call to call and do not depend on what other sequences hold;
  * their lengths may move the borders of the splits, and so the last bits.
- * Errors: EINVAL, EUNSUPPORTED (d, rows), EWORKSPACE (below
- * stepkv_cache4_decode_workspace_bytes, or not 256-byte aligned), EHIP. */
+ * Errors: EINVAL (also a scale whose product with log2(e) overflows),
+ * EUNSUPPORTED (d, rows), EWORKSPACE (below stepkv_cache4_decode_workspace_bytes,
+ * or not 256-byte aligned), EHIP. */
 int stepkv_cache4_decode(const stepkv_cache4* c, int32_t num_q_heads, const void* q_dec,
                          const int32_t* blocks, int32_t num_blocks, float scale, float* out,
                          float* lse, void* workspace, size_t ws_bytes, void* stream);

@@ -94,6 +94,8 @@ int check_attend(const stepkv_cache4* c, int32_t num_q_heads, const void* q_dec,
   const int rc = check_heads(c, num_q_heads);
   if (rc != STEPKV_OK) return rc;
   if (!q_dec || !out || !std::isfinite(scale) || !aligned(q_dec, 16)) return STEPKV_EINVAL;
+  // the kernel scales logits by scale * log2(e): 0 times an infinity is NaN
+  if (scale > 0.0f && !std::isfinite(scale * 1.44269504088896341f)) return STEPKV_EINVAL;
   return STEPKV_OK;
 }
 

@@ -99,3 +99,13 @@ def test_refuses_more_than_a_launch_takes(call):
 def test_refuses_row_offsets_that_int32_does_not_hold(cu):
     with pytest.raises((ValueError, OverflowError)):
         C4.Cache4(1, 1, 64, cu, device="cpu")
+
+
+@pytest.mark.parametrize("scale,code", [(3.0e38, B.EINVAL), (2.4e38, B.EINVAL), (2.3e38, B.EWORKSPACE),
+                                        (-3.0e38, B.EWORKSPACE)])
+def test_refuses_a_scale_that_overflows_in_the_log2_domain(scale, code):
+    """Logits of 0 would be 0 * inf there. (A misaligned workspace ends the calls that pass.)"""
+    lib, c = C4.load(), _cache([100, 3000], 2, 2)
+    ws = (FAKE + 8, 1 << 40, None)
+    assert lib.stepkv_cache4_decode(c, 8, FAKE, None, 0, scale, FAKE, None, *ws) == code
+    assert lib.stepkv_cache4_decode_sparse(c, 8, FAKE, 4, 1, 1, scale, FAKE, FAKE, None, *ws) == code
