@@ -47,7 +47,9 @@
  * Rows that hold no token are never read or written.
  * Block b of sequence s is its tokens 64 b .. 64 b + 63; k_bounds holds the
  * least (0) and greatest (1) key value per channel over the tokens that the
- * block holds (NaN where one is NaN), at block floor(cu_rows[s]/64) + s + b.
+ * block holds (NaN where one is NaN), at block floor(cu_rows[s]/64) + s + b. They
+ * are kept by the calls that write; where lens[s] was lowered by the caller, the
+ * last block's are those of its earlier tokens too (wider, and bounds still).
  */
 #ifndef STEPKV_CACHE4_H_
 #define STEPKV_CACHE4_H_
@@ -157,10 +159,12 @@ size_t stepkv_cache4_decode_workspace_bytes(const stepkv_cache4* c, int32_t num_
  * sequence, KV head); an entry that is no block of the sequence (-1), or is
  * not above every entry before it, is passed over, and so are the entries past
  * as many as the sequence has blocks.
- * A NaN in an attended key, value or query makes its results NaN. fp32 sums of
- * exact products, the probabilities in fp32. Results are
- * the same from call to call and do not depend on what other sequences hold;
- * their lengths may move the borders of the splits, and so the last bits.
+ * A NaN in an attended key, value or query makes its results NaN, and so does a
+ * logit that overflows to +inf. fp32 sums of exact products, the probabilities
+ * in fp32, up to 2^16 before they are divided by their sum: sums over values past
+ * about 2^111 may overflow. Results are the same from call to call. What other
+ * sequences hold does not enter them; how many tokens they hold may move the
+ * borders of the splits, and so change the last bits.
  * Errors: EINVAL (also a scale whose product with log2(e) overflows),
  * EUNSUPPORTED (d, rows), EWORKSPACE (below stepkv_cache4_decode_workspace_bytes,
  * or not 256-byte aligned), EHIP. */
@@ -179,8 +183,9 @@ size_t stepkv_cache4_select_workspace_bytes(const stepkv_cache4* c);
  * (q kmax where q > 0, q kmin where q < 0), an upper bound of the group's summed
  * logits in the block, computed in 64 bits; a NaN score ranks as -inf, equal
  * scores the lower block first. So a NaN in any of the group's queries, which
- * makes every score NaN, lists the lowest blocks. Written ascending to blocks int32 [L][S][H][num_blocks], -1 past the last; all the
- * blocks of a sequence that has no more than num_blocks.
+ * makes every score NaN, lists the lowest blocks. Written ascending to blocks
+ * int32 [L][S][H][num_blocks], -1 past the last; all the blocks of a sequence
+ * that has no more than num_blocks.
  * Errors: EINVAL (also a cache without k_bounds, num_blocks < 1, negative
  * counts, first_blocks + last_blocks > num_blocks), EUNSUPPORTED (d, rows),
  * EWORKSPACE, EHIP. */

@@ -5,12 +5,12 @@ of a pruning boundary) and ``append4`` (a step's new tokens), read back by ``rea
 to by ``decode_attention4`` and, over its best-scoring blocks of 64 tokens, ``decode_sparse4``.
 
     cache = Cache4(L, Hkv, d, cu_rows)            # rows that each sequence may use
+    layers = [cache.layers(l) for l in range(L)]  # once: making a view takes about 30 us
     compact4(pb, cache, k, v, idx, cu_retained)   # after select; sets cache.lens
     advance4(cache, cu_new)                       # each decode step, once:
     for l in range(L):                            # the model's layers
-        layer = cache.layers(l)
-        append4(layer, k_new[l:l + 1], v_new[l:l + 1], cu_new)
-        out = decode_attention4(layer, q[l:l + 1])
+        append4(layers[l], k_new[l:l + 1], v_new[l:l + 1], cu_new)
+        out = decode_attention4(layers[l], q[l:l + 1])
 
 Argument marshalling only; there is no CPU fallback. Every tensor of a call lies on the
 cache's device, and the call goes to the current stream of that device unless a stream of it
@@ -94,7 +94,8 @@ class Cache4:
     (copied: what is written into the given array later changes nothing).
 
     The buffers are allocated (zeroed) unless given; ``k_bounds=False`` keeps no bounds, for
-    caches whose blocks are never selected. ``lens`` (int32 [S]) counts each sequence's tokens."""
+    caches whose blocks are never selected. ``lens`` (int32 [S]) counts each sequence's tokens.
+    Given codes that hold tokens need the bounds that go with them: zeroed ones are not theirs."""
 
     def __init__(self, num_layers: int, num_kv_heads: int, head_dim: int, cu_rows, *, k_codes=None,
                  v_codes=None, k_scales=None, v_scales=None, k_bounds=True, lens=None,
@@ -150,7 +151,8 @@ class Cache4:
         self._strides = {}  # checked strides of new tokens, by their layout
 
     def layers(self, first: int, n: int = 1) -> "Cache4":
-        """Layers first .. first + n - 1 as a cache of their own (views; lens is shared)."""
+        """Layers first .. first + n - 1 as a cache of their own (views; lens is shared). A view is
+        made anew at every call: keep those of a model's layers over its steps."""
         if n < 1 or first < 0 or first + n > self.num_layers:
             raise ValueError(f"layers {first} .. {first + n - 1} of {self.num_layers}")
         v = object.__new__(Cache4)

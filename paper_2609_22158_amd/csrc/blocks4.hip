@@ -3,9 +3,10 @@
 //   sum_i a_i kmax_i + b_i kmin_i,  a = sum_g max(q_g, 0), b = sum_g min(q_g, 0),
 // which is sum_g sum_i max(q_gi kmin_i, q_gi kmax_i) with one product per
 // channel and bound whatever the group, and the threshold among them. 4d bytes
-// of bounds a block bound it. The sums are kept in 64 bits, so that two scores
-// compare as their exact values do (32-bit sums would rank close blocks by the
-// order of their additions).
+// of bounds a block bound it. The sums are kept in 64 bits and taken in one order
+// for every block: the products are exact, so are sums of values within some 2^30
+// of each other, and equal bounds give equal scores whatever their size (32-bit
+// sums would rank close blocks by their roundings).
 //
 // select4_kernel: one workgroup per (layer, sequence, KV head) scores its blocks
 // into LDS, finds the threshold by radix passes over the ordered keys and lists

@@ -205,9 +205,10 @@ __device__ __forceinline__ void store_bounds(const Cache4View& c, int lh, const 
 // bytes (8 channels) of a row, a quad of lanes a group. A token of the call
 // without a source keeps what its row holds, and the block's bounds count that
 // like the rows that are written. 32 layers x 8 heads x 1536 rows gathered from
-// 32768 take 51 us (255 MB, 5.0 TB/s), bound by the gather's reads in flight: 64
-// rows of K and V a workgroup, 32 KB. Code stores are non-temporal (with ordinary
-// ones 54 us; 16-byte stores of words exchanged within the quads 60).
+// 32768 take 52 to 54 us (255 MB, 4.7 to 4.9 TB/s), bound by the gather's reads in
+// flight: 64 rows of K and V a workgroup, 32 KB. Code stores are non-temporal
+// (measured at one time: 51 us, with ordinary ones 54, with 16-byte stores of
+// words exchanged within the quads 60).
 template <int D>
 __global__ __launch_bounds__(kThreads) void write4_kernel(Write4Args a) {
   constexpr int PR = D / 8;             // pieces of 8 channels a row
