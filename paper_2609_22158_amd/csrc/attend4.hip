@@ -38,7 +38,6 @@
 namespace stepkv {
 namespace {
 
-typedef float f32x4_t __attribute__((__vector_size__(4 * sizeof(float))));
 typedef short i16x4_t __attribute__((__vector_size__(4 * sizeof(short))));
 
 constexpr int kTile = 32;  // tokens a wave computes at a time
@@ -46,18 +45,6 @@ constexpr int kWaves = 4;  // waves of a workgroup
 constexpr int kMergeThreads = 256;  // of a merge of many rows
 constexpr float kSlack = 16.f;
 constexpr float kLog2e = 1.44269504088896341f;
-
-// The value of lane l ^ 16 and of lane l ^ 32 (permlane swaps).
-__device__ __forceinline__ float xor16(float x) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
-                                                  false);
-  return __uint_as_float(((threadIdx.x >> 4) & 1) ? r[0] : r[1]);
-}
-__device__ __forceinline__ float xor32(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
-                                                  false);
-  return __uint_as_float(((threadIdx.x >> 5) & 1) ? r[0] : r[1]);
-}
 
 // Rows that sequence s gives to the splits: its tokens, or 64 per list entry.
 // No more entries are looked at than the sequence has blocks.
@@ -106,47 +93,6 @@ __device__ __forceinline__ int v_read(int r, int j, int gp, int c) {
 }
 
 typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
-
-// Eight probabilities as bf16 operands whose sum they are, exactly: three parts
-// of 8 bits of the significand each, by truncation (the rest is exact in fp32).
-// Groups of at most 5 heads lie in the operand's 16 rows three times (C = 3), and
-// each copy takes its own part: one product instead of three (8 layers x 8 heads
-// x 131071 rows, G 4: 200 -> 187 us; two copies of at most 8 heads and two
-// products: no faster).
-template <int C>
-struct Parts {
-  static constexpr int N = 3 / C;
-  bf16x8_t x[N];
-};
-__device__ __forceinline__ uint32_t upper(uint32_t b, uint32_t a) {  // the upper halves of a, b
-  return __builtin_amdgcn_perm(b, a, 0x07060302u);
-}
-// x less its bits in mask (the upper half, or none).
-__device__ __forceinline__ uint32_t below(uint32_t x, uint32_t mask) {
-  return __float_as_uint(__uint_as_float(x) - __uint_as_float(x & mask));
-}
-template <int C>
-__device__ __forceinline__ Parts<C> split_parts(const float (&p)[8], int copy) {
-  constexpr uint32_t F = 0xffff0000u;
-  const uint32_t m1 = copy >= 1 ? F : 0u, m2 = copy >= 2 ? F : 0u;
-  u32x4_t w[Parts<C>::N];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t a = __float_as_uint(p[2 * i]), b = __float_as_uint(p[2 * i + 1]);
-    if constexpr (C == 3) {
-      w[0][i] = upper(below(below(b, m1), m2), below(below(a, m1), m2));
-    } else {
-      const uint32_t a1 = below(a, F), b1 = below(b, F);
-      w[0][i] = upper(b, a);
-      w[1][i] = upper(b1, a1);
-      w[2][i] = upper(below(b1, F), below(a1, F));
-    }
-  }
-  Parts<C> r;
-#pragma unroll
-  for (int k = 0; k < Parts<C>::N; ++k) r.x[k] = __builtin_bit_cast(bf16x8_t, w[k]);
-  return r;
-}
 
 // The reference of a wave that saw tokens, whose logits are all -inf: below every
 // logit, but not that of a wave without tokens.

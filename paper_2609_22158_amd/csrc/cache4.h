@@ -6,16 +6,12 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "launch.h"
+
 namespace stepkv {
 
 constexpr int kBlock4 = 64;  // tokens of a block (STEPKV_CACHE4_BLOCK)
 constexpr int kGroup4 = 32;  // channels of a scale (STEPKV_CACHE4_GROUP)
-
-// A launch has fewer than 2^32 threads: of more, it runs the first modulo 2^32 and
-// reports no error.
-inline bool grid_fits(int64_t workgroups, int threads) {
-  return workgroups <= (int64_t)UINT32_MAX / threads;
-}
 
 // The cache as the kernels see it.
 struct Cache4View {
