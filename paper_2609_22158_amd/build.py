@@ -20,7 +20,7 @@ C_DEMO = os.path.join(ROOT, "tests", "c_abi", "compress_demo")
 
 SOURCES = ["api.cpp", "step_text.cpp", "saliency.hip", "fewrows.hip", "fuse.hip", "select.hip", "compact.hip",
            "decode.hip", "scratch.hip", "probe.hip", "cache4_api.cpp", "cache4.hip", "attend4.hip",
-           "blocks4.hip"]
+           "blocks4.hip", "cache8_api.cpp", "cache8.hip", "attend8.hip", "evict8.hip"]
 ARCH = "gfx950"
 
 
@@ -76,7 +76,7 @@ def build(verbose: bool = False, extra_flags=(), lib_path: str = LIB) -> str:
     return lib_path
 
 
-HOST_SOURCES = ["api.cpp", "step_text.cpp", "cache4_api.cpp"]
+HOST_SOURCES = ["api.cpp", "step_text.cpp", "cache4_api.cpp", "cache8_api.cpp"]
 ASAN_LIB = os.path.join(BUILD + "_asan", "libstepkv_asan.so")
 
 

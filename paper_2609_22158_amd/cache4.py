@@ -69,6 +69,9 @@ _SIGNATURES = {
                                                    ctypes.c_float, _vp, _vp, _vp, _vp, _sz, _vp]),
 }
 
+# sizes of 256 bytes or less mean that the call takes no workspace
+_NONE_BELOW = ("stepkv_cache4_decode_workspace_bytes", "stepkv_cache8_decode_workspace_bytes")
+
 _lib: Optional[ctypes.CDLL] = None
 _fns: dict = {}  # the library's functions by name
 
@@ -78,14 +81,30 @@ def load() -> ctypes.CDLL:
     global _lib
     if _lib is None:
         lib = B.load()
-        for name, (res, args) in _SIGNATURES.items():
-            fn = getattr(lib, name)
-            fn.restype = res
-            fn.argtypes = args
-            _fns[name] = fn
+        declare(lib, _SIGNATURES)
         _fns["stepkv_status_read"] = lib.stepkv_status_read
         _lib = lib
     return _lib
+
+
+def declare(lib: ctypes.CDLL, signatures: dict) -> None:
+    """Declares functions of the library, for ``_call`` to find."""
+    for name, (res, args) in signatures.items():
+        fn = getattr(lib, name)
+        fn.restype = res
+        fn.argtypes = args
+        _fns[name] = fn
+
+
+def row_offsets(cu_rows) -> np.ndarray:
+    """A cache's own copy of its row offsets, which the library reads at every call."""
+    cu = np.array(cu_rows, dtype=np.int32, order="C")
+    cu.setflags(write=False)
+    if cu.ndim != 1 or cu.size < 2:
+        raise ValueError("cu_rows: the row offsets of one sequence or more")
+    if not np.array_equal(cu, cu_rows):
+        raise ValueError("cu_rows: offsets that int32 does not hold")
+    return cu
 
 
 # ---------------------------------------------------------------- the cache
@@ -103,12 +122,7 @@ class Cache4:
         import torch
 
         self.num_layers, self.num_kv_heads, self.head_dim = num_layers, num_kv_heads, head_dim
-        self.cu_rows = np.array(cu_rows, dtype=np.int32, order="C")  # a copy: the library reads it at every call
-        self.cu_rows.setflags(write=False)
-        if self.cu_rows.ndim != 1 or self.cu_rows.size < 2:
-            raise ValueError("cu_rows: the row offsets of one sequence or more")
-        if not np.array_equal(self.cu_rows, cu_rows):
-            raise ValueError("cu_rows: offsets that int32 does not hold")
+        self.cu_rows = row_offsets(cu_rows)
         self.num_seqs = int(self.cu_rows.size - 1)
         self.rows = int(self.cu_rows[-1])
         self.device = _device(device)
@@ -230,7 +244,7 @@ def _workspace(workspace, cache, stream, size, *args):
         nbytes = cache._sizes.get(key)
         if nbytes is None:
             nbytes = int(_fns[size](cache._ref, *args))
-            if size == "stepkv_cache4_decode_workspace_bytes" and nbytes <= 256:
+            if size in _NONE_BELOW and nbytes <= 256:
                 nbytes = 0  # none is needed
             cache._sizes[key] = nbytes
         if nbytes == 0:
@@ -316,21 +330,25 @@ def read4(cache: Cache4, cu_out, out_rows: int, *, k_out=None, v_out=None, strea
     """stepkv_cache4_read: the last cu_out[s + 1] - cu_out[s] tokens of every sequence as bf16
     rows cu_out[s] .. of k, v [L][Hkv][out_rows][d]; ``k_out=False`` or ``v_out=False`` leaves
     that one out (None in the result). Rows without a token stay as they were."""
+    return _read(cache, "stepkv_cache4_read", cu_out, out_rows, k_out, v_out, stream)
+
+
+def _read(cache, name, cu_out, out_rows, k_out, v_out, stream):
     import torch
 
     shape = (cache.num_layers, cache.num_kv_heads, int(out_rows), cache.head_dim)
     cp = _need(cu_out, torch.int32, (cache.num_seqs + 1,), "cu_out", cache.device)
 
-    def rows(t, name):
+    def rows(t, which):
         if t is False:
             return None, None
         if t is None:
             t = _empty(shape, torch.bfloat16, cache, stream)
-        p = _need(t, torch.bfloat16, shape, name, cache.device)
+        p = _need(t, torch.bfloat16, shape, which, cache.device)
         return t, p if t.numel() else None
 
     (k, kp), (v, vp) = rows(k_out, "k_out"), rows(v_out, "v_out")
-    _call(cache, "stepkv_cache4_read", stream, cache._ref, cp, int(out_rows), kp, vp)
+    _call(cache, name, stream, cache._ref, cp, int(out_rows), kp, vp)
     return k, v
 
 

@@ -1,0 +1,557 @@
+// One decode step's attention over the 8-bit cache: out = softmax(scale *
+// q . K^T) V per (layer, sequence, query head), and the weight that every token
+// has in it.
+//
+// The cache's 2 d bytes a token and KV head bound it. One conversion instruction
+// gives two exact bf16 values, the block's scale included, and both products run
+// on MFMA.
+//
+// attend8_kernel: one workgroup per (layer, KV head, 16 query heads, split of
+// a sequence's tokens), its waves on consecutive runs of 32-token tiles, each
+// with its own online softmax. Per tile and wave:
+//  - K: lane (g, r) = (l / 16, l % 16) holds 16 channels of row r at a time (those
+//    from 64 j + 16 g, j < d / 64) as the A operand of v_mfma_f32_16x16x32_bf16, 8
+//    channels a step; the query heads are the B operand in the same channel
+//    order. Lane (g, r) then holds head r's logits of rows 4 g .. 4 g + 3 of each
+//    16-row half.
+//  - softmax per head in that layout, in the log2 domain, with a reference
+//    that moves only when a logit exceeds it by kSlack.
+//  - V: the codes go into the wave's LDS tile as they are; ds_read_b64_tr_b8 gives
+//    a column's 8 rows per lane, in the order in which the lane holds P, and the
+//    conversion makes them the B operand. P is the A operand, as three bf16 parts
+//    that are it exactly (in one operand for narrow groups); the same parts times
+//    ones give the softmax's sum.
+// combine8_kernel merges the splits. To gather weights the logits are kept (4
+// bytes a query head and token, 2 to 12 % of the cache's), and gather8_kernel, or
+// the workgroup that has the whole sequence, turns them into weights once the
+// row's maximum and sum are known.
+#include "cache8_device.h"
+
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+namespace stepkv {
+namespace {
+
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2_t lds_i32x2;
+
+constexpr int kTile = 32;  // tokens a wave computes at a time
+constexpr int kWaves = 4;  // waves of a workgroup
+constexpr int kMergeThreads = 256;  // of a merge of many rows
+constexpr int kGatherThreads = 256;
+constexpr float kSlack = 16.f;
+constexpr float kLog2e = 1.44269504088896341f;
+
+// Rows of a split, from the tokens there are when the kernel runs: as many as
+// give at most a.splits splits in all, sum_s ceil(n_s / rows) <= total / rows +
+// nonempty sequences. A multiple of a tile for each of the waves.
+__device__ __forceinline__ int rows_per_split(const Attend8Args& a) {
+  const int lane = threadIdx.x & 63;
+  int64_t total = 0;
+  int some = 0, most = 0;  // most: splits of min_rows
+  for (int s0 = 0; s0 < a.c.S; s0 += kWave) {
+    const int n = s0 + lane < a.c.S ? held_tokens(a.c, s0 + lane) : 0;
+    total += (uint32_t)wave_total(wave_scan(n));  // the rooms add up to less than 2^31
+    some += __popcll(ballot(n > 0));
+    most += wave_total(wave_scan((n + a.min_rows - 1) / a.min_rows));
+  }
+  if (most <= a.splits) return a.min_rows;
+  const int slots = max(a.splits - some, 1);
+  const int64_t rows = (total + slots - 1) / slots;
+  return (int)((max(rows, (int64_t)a.min_rows) + a.min_rows - 1) / a.min_rows * a.min_rows);
+}
+
+// Byte offset of piece j (16 channels) of row r in a wave's V tile, row-major:
+// with the XORs the writes (whole rows) and the transposing reads (16 bytes of
+// each of the 16 rows that two groups of 16 lanes take) touch every bank once.
+template <int D>
+__device__ __forceinline__ int v_at(int r, int j) {
+  const int b12 = (r >> 1) & 3, b4 = (r >> 4) & 1;
+  return D == 128 ? r * 128 + 16 * (j ^ (b12 | b4 << 2))
+                  : r * 64 + 16 * (j ^ (((r >> 2) & 1) | b4 << 1));
+}
+
+// The reference of a wave that saw tokens, whose logits are all -inf: below every
+// logit, but not that of a wave without tokens.
+constexpr float kNoWeight = -3.40282347e38f;
+
+// The result of a query head from its sums (row: (layer, sequence, query head)).
+// Without a token zeros; where every logit is -inf (an overflow) the softmax of
+// such logits, 0 / 0.
+__device__ __forceinline__ void finish(const Attend8Args& a, size_t row, int ch, int D, float M,
+                                       float Z, float O) {
+  a.out[row * D + ch] = M == -INFINITY && Z == 0.f ? 0.f : O / Z;
+  if (ch != 0) return;
+  if (a.lse) a.lse[row] = Z == 0.f ? -INFINITY : (M + log2f(Z)) * 0.693147180559945309f;
+  if (a.logits && !a.single) a.norms[row] = make_float2(M, 1.f / Z);
+}
+
+// The weight of a token whose unscaled logit is y; NaN where M or 1 / Z says so.
+__device__ __forceinline__ float weight_of(float y, float cl2, float2 norm) {
+  return fast_exp2(fmaf(y, cl2, -norm.x)) * norm.y;
+}
+
+// NW waves share a split (or, with a.single, a whole sequence); C copies (1 or 3)
+// of the query heads in the operands' rows.
+template <int D, int NW, bool GATHER, int C>
+__global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(3)))
+void attend8_kernel(Attend8Args a) {
+  constexpr int KP = D / 64;        // 16-byte K pieces of a row that a lane loads
+  constexpr int NS = D / 32;        // MFMA steps of S
+  constexpr int VL = D / 32;        // 16-byte V pieces a lane loads per tile
+  constexpr int VP = D / 16;        // of a row
+  constexpr int VR = kTile / VL;    // rows between them
+  constexpr int NB = D / 16;        // 16-column blocks of O
+  constexpr int ST = D + 2;
+  constexpr int TB = kTile * D;     // bytes of a V tile
+  constexpr int kStateBytes = NW * 16 * ST * 4;
+  __shared__ __attribute__((aligned(16)))
+  uint8_t smem[NW * TB > kStateBytes ? NW * TB : kStateBytes];
+  __shared__ __attribute__((aligned(16))) float fscale[NW][16];
+  __shared__ float2 norm_s[16];
+  const Cache8View& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int g4 = lane >> 4, c16 = lane & 15;
+  if (blockIdx.x == 0 && wave == 0) report_rooms(c);
+  // Workgroups are dealt to the 8 XCDs in turn; each XCD takes a contiguous
+  // eighth of the splits.
+  const int bid = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
+  const int unit = uniform(bid / a.splits);  // (layer, KV head, 16 query heads)
+  const int gs = uniform(bid - unit * a.splits);
+  const int tiles = (a.G + 15) / 16;
+  if (unit >= c.L * c.H * tiles) return;  // the grid is padded to a multiple of 8
+  const int lh = uniform(unit / tiles), hd0 = 16 * (unit - lh * tiles);  // first head of the group
+  const int l = uniform(lh / c.H), h = lh - l * c.H;
+  int s = gs, w0, w1;  // this wave's rows [w0, w1) of those of its sequence
+  if (a.single) {
+    const int share = (held_const(c, s) + NW * kTile - 1) / (NW * kTile) * kTile;
+    w0 = wave * share;
+    w1 = w0 + share;
+  } else {
+    int first;
+    const int split = rows_per_split(a);
+    locate_item(c.S, gs, [&](int sq) { return (held_tokens(c, sq) + split - 1) / split; }, s,
+                first);
+    if (s < 0) return;  // past the last split: uniform over the workgroup
+    w0 = (gs - first) * split + wave * (split / NW);
+    w1 = w0 + split / NW;
+  }
+  s = uniform(s);
+  const int held = held_const(c, s);
+  const int t0 = uniform(w0 / kTile), t1 = uniform((min(held, w1) + kTile - 1) / kTile);  // its tiles
+  const int heads = min(a.G - hd0, 16);
+  constexpr int kCols = 16 / C;  // columns of a copy
+  const int copy = c16 / kCols, hcol = c16 % kCols;
+  bf16x8_t qb[NS];
+#pragma unroll
+  for (int ks = 0; ks < NS; ++ks) {
+    qb[ks] = bf16x8_t{};
+    if (hcol < heads && copy < C)
+      qb[ks] = *reinterpret_cast<const bf16x8_t*>(
+          a.q + (((size_t)l * c.S + s) * a.Hq + h * a.G + hd0 + hcol) * D + 64 * (ks / 2) +
+          16 * g4 + 8 * (ks % 2));
+  }
+  const float cl2 = a.scale * kLog2e;
+  float m_ref = -INFINITY;
+  f32x4_t o[NB], z = f32x4_t{};
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) o[nb] = f32x4_t{};
+  const int seq_row = read_const(c.cu_rows, s);
+  const size_t row0 = (size_t)lh * c.rows + seq_row;
+  const size_t blk0 = (size_t)lh * c.nblk + first_block(seq_row, s);
+  uint8_t* const vt = smem + wave * TB;
+  const int vrow = lane / VP, vpiece = lane % VP;  // this lane's V row and piece
+  // the logits of this lane's head, from the sequence's first row
+  float* const zrow = GATHER ? a.logits + ((size_t)unit * min(a.G, 16) + hcol) * c.rows + seq_row
+                             : nullptr;
+
+  struct Tile {
+    u32x4_t k[2][KP], v[VL];
+    float ks, vs;
+  };
+  // Loads tile t (or, past the end, again the last one, so that the count of
+  // loads in flight is the same in every round).
+  auto load = [&](Tile& x, int t) __attribute__((always_inline)) {
+    const int b = min(t, t1 - 1) * kTile, last = held - 1 - b;
+    const uint8_t* __restrict__ kc = c.k_codes + (row0 + b) * D;
+    const uint8_t* __restrict__ vc = c.v_codes + (row0 + b) * D;
+    x.ks = read_const(c.k_scales, blk0 + b / kBlock8);
+    x.vs = read_const(c.v_scales, blk0 + b / kBlock8);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint32_t r = min(16 * u + c16, last);  // rows past the end: the last one again
+#pragma unroll
+      for (int j = 0; j < KP; ++j)
+        x.k[u][j] = __builtin_nontemporal_load(
+            reinterpret_cast<const u32x4_t*>(kc + (r * D + 64 * j + 16 * g4)));
+    }
+#pragma unroll
+    for (int u = 0; u < VL; ++u) {
+      const uint32_t r = min(VR * u + vrow, last);
+      x.v[u] = __builtin_nontemporal_load(
+          reinterpret_cast<const u32x4_t*>(vc + (r * D + 16 * vpiece)));
+    }
+  };
+  // The first half of a tile's work, after which its registers are free: the
+  // logits on the matrix cores, V's codes in LDS.
+  f32x4_t acc[2];
+  auto consume = [&](const Tile& x) __attribute__((always_inline)) {
+    acc[0] = acc[1] = f32x4_t{};
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int ks = 0; ks < NS; ++ks)
+        acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            __builtin_bit_cast(bf16x8_t, spread8(x.k[u][ks / 2][2 * (ks % 2)],
+                                                 x.k[u][ks / 2][2 * (ks % 2) + 1], x.ks)),
+            qb[ks], acc[u], 0, 0, 0);
+#pragma unroll
+    for (int u = 0; u < VL; ++u)
+      *reinterpret_cast<u32x4_t*>(vt + v_at<D>(VR * u + vrow, vpiece)) = x.v[u];
+  };
+  auto attend = [&](int tok, float vs) __attribute__((always_inline)) {
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = acc[i >> 2][i & 3];
+    if constexpr (GATHER) {
+      if (c16 < heads) {  // the first copy's lanes; rows past the sequence's have no place
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int j = tok + 16 * u + 4 * g4;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (j + i < held) zrow[j + i] = y[4 * u + i];
+        }
+      }
+    }
+    if (tok + kTile > held) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (tok + 16 * (i >> 2) + 4 * g4 + (i & 3) >= held) y[i] = -INFINITY;
+    }
+    float tmax = y[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) tmax = fmaxf(tmax, y[i]);
+    tmax *= cl2;  // the scale is positive
+    if (__builtin_amdgcn_ballot_w64(tmax > m_ref + kSlack) != 0) {  // wave-uniform, rare
+      tmax = fmaxf(tmax, xor16(tmax));
+      tmax = fmaxf(tmax, xor32(tmax));
+      const float m_new = tmax > m_ref + kSlack ? tmax : m_ref;
+      const float f = m_ref == -INFINITY ? 0.f : fast_exp2(m_ref - m_new);
+      m_ref = m_new;
+      if (g4 == 0) fscale[wave][c16] = f;
+      __builtin_amdgcn_wave_barrier();
+      const float4 f4 = *reinterpret_cast<const float4*>(&fscale[wave][4 * g4]);
+      z[0] *= f4.x;
+      z[1] *= f4.y;
+      z[2] *= f4.z;
+      z[3] *= f4.w;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        o[nb][0] *= f4.x;
+        o[nb][1] *= f4.y;
+        o[nb][2] *= f4.z;
+        o[nb][3] *= f4.w;
+      }
+    }
+    // a logit of -inf has no weight, also while the reference is still -inf
+    const float m = m_ref == -INFINITY ? 0.f : m_ref;
+    float p[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = fast_exp2(fmaf(y[i], cl2, -m));
+    const Parts<C> pp = split_parts<C>(p, copy);
+    const bf16x8_t one = __builtin_bit_cast(bf16x8_t, u32x4_t{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+#pragma unroll
+    for (int k = 0; k < Parts<C>::N; ++k) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pp.x[k], one, z, 0, 0, 0);
+    // column block nb: lane (g, c) gets column c of rows 4 g .. 4 g + 3 of both halves
+    const int vr = c16 < 8 ? 4 * g4 + (c16 >> 1) : 16 + 4 * g4 + (c16 >> 1) - 4;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const i32x2_t w =
+          __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(vt + v_at<D>(vr, nb) + 8 * (c16 & 1)));
+      const bf16x8_t vb = __builtin_bit_cast(bf16x8_t, spread8((uint32_t)w[0], (uint32_t)w[1], vs));
+#pragma unroll
+      for (int k = 0; k < Parts<C>::N; ++k)
+        o[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pp.x[k], vb, o[nb], 0, 0, 0);
+    }
+  };
+  if (t0 < t1) {
+    Tile cur;
+    load(cur, t0);
+    for (int t = t0; t < t1; ++t) {  // wave-uniform
+      const float vs = cur.vs;
+      consume(cur);
+      load(cur, t + 1);
+      attend(t * kTile, vs);
+    }
+  }
+  __syncthreads();  // the states overwrite the V tiles of every wave
+  auto state = reinterpret_cast<float(*)[16][ST]>(smem);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((4 * g4 + i) % kCols < heads && (4 * g4 + i) / kCols < C) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) state[wave][4 * g4 + i][16 * nb + c16] = o[nb][i];
+      if (c16 == 0) state[wave][4 * g4 + i][D + 1] = z[i];
+    }
+  }
+  if (g4 == 0 && c16 < heads)  // the same in every copy
+    state[wave][c16][D] = t0 < t1 ? fmaxf(m_ref, kNoWeight) : -INFINITY;
+  __syncthreads();
+  float* const part = a.partial + ((size_t)unit * a.splits + gs) * min(a.G, 16) * ST;
+  const size_t row_out = ((size_t)l * c.S + s) * a.Hq + h * a.G + hd0;
+  for (int e = tid; e < heads * D; e += NW * kWave) {
+    const int hd = e / D, ch = e - hd * D;
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, state[w][hd][D]);
+    float Z = 0.f, O = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float m = state[w][hd][D];
+      const float x = m == -INFINITY ? 0.f : fast_exp2(m - M);  // a NaN sum stays NaN
+      float z1 = state[w][hd][D + 1], o1 = state[w][hd][ch];
+#pragma unroll
+      for (int k = 1; k < C; ++k) {
+        z1 += state[w][k * kCols + hd][D + 1];
+        o1 += state[w][k * kCols + hd][ch];
+      }
+      Z = fmaf(z1, x, Z);
+      O = fmaf(o1, x, O);
+    }
+    if (a.single) {
+      finish(a, row_out + hd, ch, D, M, Z, O);
+      if (GATHER && ch == 0) norm_s[hd] = make_float2(M, 1.f / Z);
+      continue;
+    }
+    part[hd * ST + ch] = O;
+    if (ch == 0) {
+      part[hd * ST + D] = M;
+      part[hd * ST + D + 1] = Z;
+    }
+  }
+  if constexpr (GATHER) {
+    // The whole sequence's logits, by this workgroup's waves: the weights, unless
+    // other workgroups have other heads of the same KV head.
+    if (!a.single) return;
+    __threadfence_block();
+    __syncthreads();
+    if (tiles > 1) {
+      if (tid < heads) a.norms[row_out + tid] = norm_s[tid];
+      return;
+    }
+    const float* __restrict__ base = a.logits + (size_t)unit * min(a.G, 16) * c.rows + seq_row;
+    for (int j = tid; j < held; j += NW * kWave) {
+      float w = 0.f;
+      for (int g = 0; g < heads; ++g)
+        w += weight_of(__hip_atomic_load(base + (size_t)g * c.rows + j, __ATOMIC_RELAXED,
+                                         __HIP_MEMORY_SCOPE_WORKGROUP), cl2, norm_s[g]);
+      c.weights[row0 + j] += w;
+    }
+  }
+}
+
+// out and lse of a (layer, sequence, KV head, 16 query heads), or of one query
+// head of them: the splits' states merged by a running maximum, four in flight
+// per thread. A thread per (head, channel), or with one head a group of
+// THREADS / D threads per channel over the splits, merged in order.
+template <int D, int THREADS, bool ONE>
+__global__ __launch_bounds__(THREADS) void combine8_kernel(Attend8Args a) {
+  constexpr int ST = D + 2;
+  constexpr int J = ONE ? THREADS / D : 1;
+  constexpr int kAhead = 4;
+  __shared__ float om[J][D], mm[J], zm[J];
+  const Cache8View& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int tiles = (a.G + 15) / 16, per = min(a.G, 16);
+  int at = blockIdx.x, g0 = 0;
+  if (ONE) {
+    g0 = uniform(at % per);
+    at = uniform(at / per);
+  }
+  const int unit = uniform(at / c.S), s = at - unit * c.S;
+  const int lh = unit / tiles, hd0 = 16 * (unit - lh * tiles) + g0;
+  const int heads = ONE ? 1 : min(a.G - hd0, 16);
+  if (hd0 >= a.G) return;  // the last tile may be narrower: uniform
+  const int split = rows_per_split(a);
+  int first = 0;  // splits of the sequences before s
+  for (int s0 = 0; s0 < s; s0 += kWave)
+    first += wave_total(
+        wave_scan(s0 + lane < s ? (held_tokens(c, s0 + lane) + split - 1) / split : 0));
+  first = min(first, a.splits);
+  const int n = min((held_const(c, s) + split - 1) / split, a.splits - first);
+  const size_t stride = (size_t)per * ST;
+  const float* __restrict__ base =
+      a.partial + ((size_t)unit * a.splits + first) * stride + (size_t)g0 * ST;
+  const int l = lh / c.H, h = lh - l * c.H;
+  const size_t row = ((size_t)l * c.S + s) * a.Hq + h * a.G + hd0;
+  const int jg = ONE ? tid / D : 0;
+  for (int e = ONE ? tid % D : tid; e < heads * D; e += THREADS) {
+    const int hd = e / D, ch = e - hd * D;
+    const float* __restrict__ p = base + (size_t)hd * ST;
+    float M = -INFINITY, Z = 0.f, O = 0.f;
+    for (int j0 = jg; j0 < n; j0 += J * kAhead) {
+      float m[kAhead], z[kAhead], o[kAhead];
+      float top = M;
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int j = min(j0 + J * u, n - 1);
+        m[u] = p[j * stride + D];
+        z[u] = p[j * stride + D + 1];
+        o[u] = p[j * stride + ch];
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (j0 + J * u >= n) m[u] = -INFINITY, z[u] = o[u] = 0.f;
+        top = fmaxf(top, m[u]);
+      }
+      const float f = M == -INFINITY ? 0.f : fast_exp2(M - top);
+      Z *= f;  // a NaN sum stays NaN
+      O *= f;
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const float x = m[u] == -INFINITY ? 0.f : fast_exp2(m[u] - top);
+        Z = fmaf(z[u], x, Z);
+        O = fmaf(o[u], x, O);
+      }
+      M = top;
+    }
+    if constexpr (ONE) {
+      om[jg][ch] = O;
+      if (ch == 0) {
+        mm[jg] = M;
+        zm[jg] = Z;
+      }
+    } else {
+      finish(a, row + hd, ch, D, M, Z, O);
+    }
+  }
+  if constexpr (ONE) {
+    __syncthreads();
+    if (tid >= D) return;
+    float M = -INFINITY, Z = 0.f, O = 0.f;
+#pragma unroll
+    for (int j = 0; j < J; ++j) M = fmaxf(M, mm[j]);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const float x = mm[j] == -INFINITY ? 0.f : fast_exp2(mm[j] - M);
+      Z = fmaf(zm[j], x, Z);
+      O = fmaf(om[j][tid], x, O);
+    }
+    finish(a, row, tid, D, M, Z, O);
+  }
+}
+
+// weights += the tokens' weights, a thread per token: the sum over the group's
+// heads in their order.
+__global__ __launch_bounds__(kGatherThreads) void gather8_kernel(Attend8Args a) {
+  const Cache8View& c = a.c;
+  const int per = c.rows / kGatherThreads + c.S;  // chunks that a (layer, KV head) may have
+  const int lh = uniform(blockIdx.x / per), at = uniform(blockIdx.x - lh * per);
+  int s, first;
+  locate_item(c.S, at, [&](int sq) { return (held_tokens(c, sq) + kGatherThreads - 1) / kGatherThreads; },
+              s, first);
+  if (s < 0) return;
+  s = uniform(s);
+  const int j = (at - first) * kGatherThreads + (int)threadIdx.x;
+  if (j >= held_const(c, s)) return;
+  const int l = uniform(lh / c.H), h = lh - l * c.H;
+  const int seq_row = read_const(c.cu_rows, s), tiles = (a.G + 15) / 16, wide = min(a.G, 16);
+  const float cl2 = a.scale * kLog2e;
+  const float2* __restrict__ norms = a.norms + ((size_t)l * c.S + s) * a.Hq + h * a.G;
+  const float* __restrict__ z = a.logits + (size_t)lh * tiles * wide * c.rows + seq_row + j;
+  float w = 0.f;
+#pragma unroll 4
+  for (int g = 0; g < a.G; ++g) w += weight_of(z[(size_t)g * c.rows], cl2, norms[g]);
+  c.weights[(size_t)lh * c.rows + seq_row + j] += w;
+}
+
+int64_t units_of(const Attend8Args& a) { return (int64_t)a.c.L * a.c.H * ((a.G + 15) / 16); }
+int64_t gather_workgroups(const Attend8Args& a) {
+  return (int64_t)a.c.L * a.c.H * (a.c.rows / kGatherThreads + a.c.S);
+}
+
+}  // namespace
+
+// Splits for the rooms. Short sequences are one split each, which needs no merge;
+// 8 waves share it while there are at most 256. Otherwise about 4096 rows a
+// split, but enough splits for four workgroups on each of the 256 compute units
+// while those have a tile per wave.
+void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host) {
+  const int64_t units = units_of(a);
+  a.min_rows = kTile * kWaves;
+  int64_t total = 0, most = 0, longest = 0;
+  for (int s = 0; s < a.c.S; ++s) {
+    const int64_t n = cu_rows_host[s + 1] - cu_rows_host[s];
+    total += n;
+    longest = std::max(longest, n);
+    most += (n + a.min_rows - 1) / a.min_rows;
+  }
+  const int64_t rows = units * a.c.S;  // workgroups of one split a sequence
+  const int64_t most_single = rows > 256 ? 1024 : std::min<int64_t>(2048, 640 + 12 * rows);
+  a.single = longest * (a.c.d + 64) / 192 <= most_single;
+  if (a.single) {
+    a.splits = a.c.S;
+    return;
+  }
+  const int64_t want = std::max<int64_t>((1024 + units - 1) / units, total / 4096);
+  a.splits = (int)std::max<int64_t>(std::min<int64_t>(most, want + a.c.S), 1);
+}
+
+size_t attend8_partial_floats(const Attend8Args& a) {
+  if (a.single) return 0;
+  return (size_t)units_of(a) * a.splits * std::min(a.G, 16) * (a.c.d + 2);
+}
+
+bool attend8_fits(const Attend8Args& a, bool gather) {
+  // 8 waves a workgroup only where there are few; the merge's where there are many
+  return grid_fits((units_of(a) * a.splits + 7) / 8 * 8, kWaves * kWave) &&
+         (a.single || grid_fits(units_of(a) * a.c.S, kMergeThreads)) &&
+         (!gather || grid_fits(gather_workgroups(a), kGatherThreads));
+}
+
+namespace {
+
+template <int D>
+void launch_attend(const Attend8Args& a, hipStream_t st) {
+  const unsigned units = (unsigned)units_of(a);
+  const dim3 grid((units * (unsigned)a.splits + 7u) / 8u * 8u);
+  auto copies = [&](auto nw, auto cc) {
+    constexpr int NW = decltype(nw)::value, C = decltype(cc)::value;
+    if (a.logits)
+      hipLaunchKernelGGL((attend8_kernel<D, NW, true, C>), grid, dim3(NW * kWave), 0, st, a);
+    else
+      hipLaunchKernelGGL((attend8_kernel<D, NW, false, C>), grid, dim3(NW * kWave), 0, st, a);
+  };
+  auto run = [&](auto nw) {
+    if (a.G <= 5) copies(nw, std::integral_constant<int, 3>{});
+    else copies(nw, std::integral_constant<int, 1>{});
+  };
+  if (a.single && grid.x <= 256) run(std::integral_constant<int, 8>{});
+  else run(std::integral_constant<int, kWaves>{});
+  if (!a.single) {
+    const unsigned rows = units * (unsigned)a.c.S;
+    if (rows >= 512)
+      hipLaunchKernelGGL((combine8_kernel<D, kMergeThreads, false>), dim3(rows), dim3(kMergeThreads),
+                         0, st, a);
+    else
+      hipLaunchKernelGGL((combine8_kernel<D, 512, true>), dim3(rows * std::min(a.G, 16)), dim3(512),
+                         0, st, a);
+  }
+  if (a.logits && (!a.single || a.G > 16))
+    hipLaunchKernelGGL(gather8_kernel, dim3((unsigned)gather_workgroups(a)), dim3(kGatherThreads), 0,
+                       st, a);
+}
+
+}  // namespace
+
+hipError_t launch_attend8(const Attend8Args& a, hipStream_t st) {
+  if (a.c.d == 128) launch_attend<128>(a, st);
+  else launch_attend<64>(a, st);
+  return hipGetLastError();
+}
+
+}  // namespace stepkv
