@@ -91,6 +91,7 @@ struct Evict8Args {
                              // from cu_rows[s] / 2 (it moves no more than half of its room)
   int keep, first, recent;
   int workers;               // waves that move rows of a (layer, KV head, sequence)
+  int longest;               // rows of the longest room
 };
 void plan_evict8(Evict8Args& a, const int32_t* cu_rows_host);
 bool evict8_fits(const Evict8Args& a);
