@@ -89,6 +89,17 @@ __device__ __forceinline__ void finish(const Attend8Args& a, size_t row, int ch,
   if (a.logits && !a.single) a.norms[row] = make_float2(M, 1.f / Z);
 }
 
+// The logits are kept by tiles of 32 tokens, [L*H*tiles][rows / 32 + S][min(G, 16)][32]:
+// a wave writes a tile in one piece. Offset of those of a unit and a sequence.
+__device__ __forceinline__ size_t logits_at(const Attend8Args& a, int unit, int seq_row, int s) {
+  const size_t tiles = a.c.rows / kTile + a.c.S;
+  return ((size_t)unit * tiles + seq_row / kTile + s) * min(a.G, 16) * kTile;
+}
+// Of token j, head 0, from there; those of the next heads follow at kTile.
+__device__ __forceinline__ size_t token_at(const Attend8Args& a, int j) {
+  return (size_t)(j / kTile) * min(a.G, 16) * kTile + j % kTile;
+}
+
 // The weight of a token whose unscaled logit is y; NaN where M or 1 / Z says so.
 __device__ __forceinline__ float weight_of(float y, float cl2, float2 norm) {
   return fast_exp2(fmaf(y, cl2, -norm.x)) * norm.y;
@@ -164,9 +175,8 @@ void attend8_kernel(Attend8Args a) {
   const size_t blk0 = (size_t)lh * c.nblk + first_block(seq_row, s);
   uint8_t* const vt = smem + wave * TB;
   const int vrow = lane / VP, vpiece = lane % VP;  // this lane's V row and piece
-  // the logits of this lane's head, from the sequence's first row
-  float* const zrow = GATHER ? a.logits + ((size_t)unit * min(a.G, 16) + hcol) * c.rows + seq_row
-                             : nullptr;
+  // the logits of this lane's head and rows, from the sequence's first tile
+  float* const zt = GATHER ? a.logits + logits_at(a, unit, seq_row, s) + c16 * kTile + 4 * g4 : nullptr;
 
   struct Tile {
     u32x4_t k[2][KP], v[VL];
@@ -216,17 +226,6 @@ void attend8_kernel(Attend8Args a) {
     float y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = acc[i >> 2][i & 3];
-    if constexpr (GATHER) {
-      if (c16 < heads) {  // the first copy's lanes; rows past the sequence's have no place
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int j = tok + 16 * u + 4 * g4;
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (j + i < held) zrow[j + i] = y[4 * u + i];
-        }
-      }
-    }
     if (tok + kTile > held) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -284,6 +283,12 @@ void attend8_kernel(Attend8Args a) {
     for (int t = t0; t < t1; ++t) {  // wave-uniform
       const float vs = cur.vs;
       consume(cur);
+      // before the loads, whose wait then is for nothing else
+      if (GATHER && c16 < heads) {  // the first copy's lanes; a tile has room for all its rows
+        f32x4_t* const z4 = reinterpret_cast<f32x4_t*>(zt + (size_t)t * min(a.G, 16) * kTile);
+        z4[0] = acc[0];
+        z4[4] = acc[1];
+      }
       load(cur, t + 1);
       attend(t * kTile, vs);
     }
@@ -343,11 +348,11 @@ void attend8_kernel(Attend8Args a) {
       if (tid < heads) a.norms[row_out + tid] = norm_s[tid];
       return;
     }
-    const float* __restrict__ base = a.logits + (size_t)unit * min(a.G, 16) * c.rows + seq_row;
+    const float* __restrict__ base = a.logits + logits_at(a, unit, seq_row, s);
     for (int j = tid; j < held; j += NW * kWave) {
       float w = 0.f;
       for (int g = 0; g < heads; ++g)
-        w += weight_of(__hip_atomic_load(base + (size_t)g * c.rows + j, __ATOMIC_RELAXED,
+        w += weight_of(__hip_atomic_load(base + token_at(a, j) + g * kTile, __ATOMIC_RELAXED,
                                          __HIP_MEMORY_SCOPE_WORKGROUP), cl2, norm_s[g]);
       c.weights[row0 + j] += w;
     }
@@ -459,13 +464,16 @@ __global__ __launch_bounds__(kGatherThreads) void gather8_kernel(Attend8Args a) 
   const int j = (at - first) * kGatherThreads + (int)threadIdx.x;
   if (j >= held_const(c, s)) return;
   const int l = uniform(lh / c.H), h = lh - l * c.H;
-  const int seq_row = read_const(c.cu_rows, s), tiles = (a.G + 15) / 16, wide = min(a.G, 16);
+  const int seq_row = read_const(c.cu_rows, s), tiles = (a.G + 15) / 16;
   const float cl2 = a.scale * kLog2e;
   const float2* __restrict__ norms = a.norms + ((size_t)l * c.S + s) * a.Hq + h * a.G;
-  const float* __restrict__ z = a.logits + (size_t)lh * tiles * wide * c.rows + seq_row + j;
   float w = 0.f;
+  for (int t = 0; t < tiles; ++t) {
+    const float* __restrict__ z = a.logits + logits_at(a, lh * tiles + t, seq_row, s) + token_at(a, j);
+    const int heads = min(a.G - 16 * t, 16);
 #pragma unroll 4
-  for (int g = 0; g < a.G; ++g) w += weight_of(z[(size_t)g * c.rows], cl2, norms[g]);
+    for (int g = 0; g < heads; ++g) w += weight_of(z[g * kTile], cl2, norms[16 * t + g]);
+  }
   c.weights[(size_t)lh * c.rows + seq_row + j] += w;
 }
 
@@ -504,6 +512,10 @@ void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host) {
 size_t attend8_partial_floats(const Attend8Args& a) {
   if (a.single) return 0;
   return (size_t)units_of(a) * a.splits * std::min(a.G, 16) * (a.c.d + 2);
+}
+
+size_t attend8_logits(const Attend8Args& a) {
+  return (size_t)units_of(a) * (a.c.rows / kTile + a.c.S) * std::min(a.G, 16) * kTile;
 }
 
 bool attend8_fits(const Attend8Args& a, bool gather) {

@@ -62,7 +62,7 @@ struct Attend8Args {
   float* out;                // [L][S][Hq][d]
   float* lse;                // [L][S][Hq] or null
   float* partial;            // [L*H*tiles][splits][min(G, 16)][d+2]: o, m (log2), z
-  float* logits;             // gather: [L*H*tiles][min(G, 16)][rows], unscaled, or null
+  float* logits;             // gather: the logits, unscaled, by tiles of tokens; or null
   float2* norms;             // gather: [L][S][Hq] reference (log2) and 1 / sum
   int Hq, G;
   int splits;                // split slots of a (layer, KV head)
@@ -73,6 +73,7 @@ struct Attend8Args {
 // Fills splits, min_rows and single from the shape and the rooms of the sequences.
 void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host);
 size_t attend8_partial_floats(const Attend8Args& a);
+size_t attend8_logits(const Attend8Args& a);  // floats of them
 bool attend8_fits(const Attend8Args& a, bool gather);
 hipError_t launch_attend8(const Attend8Args& a, hipStream_t st);
 

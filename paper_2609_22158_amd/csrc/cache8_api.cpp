@@ -96,8 +96,7 @@ size_t partial_bytes(const Attend8Args& a) {
   return align_up(sizeof(float) * attend8_partial_floats(a));
 }
 size_t logits_bytes(const Attend8Args& a) {
-  const size_t heads = (size_t)a.c.L * a.c.H * ((a.G + 15) / 16) * std::min(a.G, 16);
-  return align_up(sizeof(float) * heads * a.c.rows);
+  return align_up(sizeof(float) * attend8_logits(a));
 }
 size_t norms_bytes(const Attend8Args& a) {
   return align_up(sizeof(float2) * (size_t)a.c.L * a.c.S * a.Hq);

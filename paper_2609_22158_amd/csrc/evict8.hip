@@ -38,12 +38,16 @@ __device__ __forceinline__ uint32_t order_key(float p) {
   return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
+constexpr int kList = 256;  // keys of one bin that are ranked by comparing them all
+
 template <int W>
 struct Scratch8 {
   uint32_t hist[kBins];
+  __attribute__((aligned(16))) uint32_t list[kList];
   uint32_t total[W];
   int count[3][W];   // of every wave: rows to be freed, rows that move, ties
-  uint32_t found[3];  // bin, rank within it, keys in it
+  uint32_t found[3];  // bin, rank within it, keys in it; then key, rank, keys equal to it
+  uint32_t listed;
 };
 
 // The bin of sh.hist that holds the rank-th greatest key (and clears sh.hist):
@@ -53,15 +57,14 @@ template <int W>
 __device__ __forceinline__ void find_bin(Scratch8<W>& sh, uint32_t rank) {
   constexpr int PB = kBins / (W * kWave);
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const int top = kBins - 1 - PB * tid;
+  const int low = kBins - PB - PB * tid;
   uint32_t n[PB], own = 0u;
+  uint32_t* const h = sh.hist + low;
+  __builtin_memcpy(n, h, sizeof(n));
+  const uint32_t zero[PB] = {};
+  __builtin_memcpy(h, zero, sizeof(n));
 #pragma unroll
-  for (int i = 0; i < PB; ++i) {
-    n[i] = sh.hist[top - i];
-    own += n[i];
-  }
-#pragma unroll
-  for (int i = 0; i < PB; ++i) sh.hist[top - i] = 0u;
+  for (int i = 0; i < PB; ++i) own += n[i];
   const uint32_t incl = (uint32_t)wave_scan((int)own);
   if (lane == kWave - 1) sh.total[wave] = incl;
   __syncthreads();
@@ -70,11 +73,12 @@ __device__ __forceinline__ void find_bin(Scratch8<W>& sh, uint32_t rank) {
   for (int v = 0; v < W; ++v) above += v < wave ? sh.total[v] : 0u;
   if (above < rank && rank <= above + own) {
 #pragma unroll
-    for (int i = 0; i < PB; ++i) {
+    for (int i = PB - 1; i >= 0; --i) {
       if (above < rank && rank <= above + n[i]) {
-        sh.found[0] = (uint32_t)(top - i);
+        sh.found[0] = (uint32_t)(low + i);
         sh.found[1] = rank - above;
         sh.found[2] = n[i];
+        sh.listed = 0u;
       }
       above += n[i];
     }
@@ -82,24 +86,13 @@ __device__ __forceinline__ void find_bin(Scratch8<W>& sh, uint32_t rank) {
   __syncthreads();
 }
 
-// Adds one to the bin of every lane with `in`: lanes of one bin as one, where they
-// are many (equal weights; atomics on one word run one after another).
-__device__ __forceinline__ void add_to_bins(uint32_t* hist, bool in, uint32_t bin, int lane) {
-  const uint64_t active = ballot(in);
-  if (active == 0ull) return;
-  const int lead = __builtin_ctzll(active);
-  const uint64_t same = ballot(in && bin == (uint32_t)__builtin_amdgcn_readlane((int)bin, lead));
-  if (__popcll(same) >= 8) {  // uniform
-    if (lane == lead) atomicAdd(&hist[bin], (uint32_t)__popcll(same));
-    in = in && !(same >> lane & 1ull);
-  }
-  if (in) atomicAdd(&hist[bin], 1u);
-}
-
-// W waves, NB keys a lane (STREAM: read again in every phase, NB at a time).
-template <int W, int NB, bool STREAM>
-__global__ __launch_bounds__(W * kWave) void evict8_kernel(Evict8Args a) {
-  __shared__ Scratch8<W> sh;
+// W waves, NG groups of 4 keys a lane: a group is 256 consecutive rows of a wave's,
+// four a lane (STREAM: read again in every phase, NG groups at a time).
+template <int W, int NG, bool STREAM>
+__global__ __launch_bounds__(W * kWave) __attribute__((amdgpu_waves_per_eu(4)))
+void evict8_kernel(Evict8Args a) {
+  constexpr int kGroup = 4 * kWave;
+  __shared__ __attribute__((aligned(16))) Scratch8<W> sh;
   const Cache8View& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   if (blockIdx.x == 0 && wave == 0) report_rooms(c);
@@ -112,131 +105,202 @@ __global__ __launch_bounds__(W * kWave) void evict8_kernel(Evict8Args a) {
     return;
   }
   const int row0 = read_const(c.cu_rows, s);
-  const float* __restrict__ w = c.weights + (size_t)lh * c.rows + row0;
-  const int32_t* __restrict__ pos = c.positions + (size_t)lh * c.rows + row0;
-  const int64_t recent = (int64_t)read_const(c.seen, s) - a.recent;  // from this position on
+  const size_t edge = (size_t)lh * c.nblk + first_block(row0, s) + keep / kBlock8;
+  const float k_edge = read_const(c.k_scales, edge), v_edge = read_const(c.v_scales, edge);
+  const char* __restrict__ w = reinterpret_cast<const char*>(c.weights + (size_t)lh * c.rows + row0);
+  const char* __restrict__ pos = reinterpret_cast<const char*>(c.positions + (size_t)lh * c.rows + row0);
+  // Positions that may go: first .. first + width - 1, where position - first, taken
+  // as unsigned, is below width (a position below `first` wraps to 2^31 and above).
+  const int64_t recent = (int64_t)read_const(c.seen, s) - a.recent;
+  const uint32_t width = (uint32_t)max(recent - a.first, (int64_t)0);
   const bool some_stay = a.first > 0 || a.recent > 0;
-  // this wave's rows: nb groups of 64 from row j0
-  const int nb = (n + W * kWave - 1) / (W * kWave);
-  const int j0 = wave * nb * kWave;
-  constexpr int kBatch = NB < 8 ? NB : 8;  // loads in flight
-  uint32_t keys[NB];
-  auto load = [&](int b0, int count) __attribute__((always_inline)) {  // groups b0 .. of this wave
-#pragma unroll
-    for (int b = 0; b < NB; b += kBatch) {
-      if (b >= count) {  // uniform
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) keys[b + i] = 0u;
-        continue;
-      }
-      float x[kBatch];
-      int p[kBatch];
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        const int j = min(j0 + (b0 + b + i) * kWave + lane, n - 1);
-        x[i] = w[j];
-        p[i] = some_stay ? pos[j] : 0;
-      }
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        const int j = j0 + (b0 + b + i) * kWave + lane;
-        const bool stays = some_stay && (p[i] < a.first || p[i] >= recent);
-        keys[b + i] = b + i < count && j < n ? (stays ? kStays : order_key(x[i])) : 0u;
-      }
-    }
-  };
-  // f(group, key) over this wave's rows, in their order
-  auto each = [&](auto&& f) __attribute__((always_inline)) {
-    if constexpr (STREAM) {
-      for (int b0 = 0; b0 < nb; b0 += NB) {
-        load(b0, nb - b0);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) f(b0 + b, keys[b]);
-      }
+  // this wave's rows: ng groups from row j0
+  const int ng = (n + W * kGroup - 1) / (W * kGroup);
+  const int j0 = wave * ng * kGroup;
+  uint32_t keys[4 * NG];
+  // the keys of a group, whose first row of this lane is j; 0 for rows past the sequence
+  auto load = [&](int j, uint32_t* k) __attribute__((always_inline)) {
+    float x[4];
+    int p[4] = {};
+    if (j - 4 * lane + kGroup <= n) {  // uniform; 32-bit byte offsets: there are less than 2^30 rows
+      __builtin_memcpy(x, w + 4u * (uint32_t)j, 16);
+      if (some_stay) __builtin_memcpy(p, pos + 4u * (uint32_t)j, 16);
     } else {
 #pragma unroll
-      for (int b = 0; b < NB; b += kBatch) {
-        if (b >= nb) break;  // uniform
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) f(b + i, keys[b + i]);
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t at = 4u * (uint32_t)min(j + e, n - 1);
+        x[e] = *reinterpret_cast<const float*>(w + at);
+        if (some_stay) p[e] = *reinterpret_cast<const int*>(pos + at);
       }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      k[e] = some_stay && (uint32_t)(p[e] - a.first) >= width ? kStays : order_key(x[e]);
+      if (j + e >= n) k[e] = 0u;
     }
   };
-  if constexpr (!STREAM) load(0, nb);
+  // f(first row of the group, its keys) over this wave's groups, in the rows' order
+  auto each = [&](auto&& f) __attribute__((always_inline)) {
+    if constexpr (STREAM) {
+      for (int g = 0; g < ng; g += NG) {
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+          if (g + i < ng) load(j0 + (g + i) * kGroup + 4 * lane, keys + 4 * i);
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+          if (g + i < ng) f(j0 + (g + i) * kGroup, keys + 4 * i);
+      }
+    } else {
+      // compares made anew in every phase, not masks held across them
+#pragma unroll
+      for (int j = 0; j < 4 * NG; ++j) asm volatile("" : "+v"(keys[j]));
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+        if (g < ng) f(j0 + g * kGroup, keys + 4 * g);  // uniform
+    }
+  };
+  if constexpr (!STREAM) {
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+      if (g < ng) load(j0 + g * kGroup + 4 * lane, keys + 4 * g);
+  }
   for (int i = tid; i < kBins; i += W * kWave) sh.hist[i] = 0u;
   __syncthreads();
-  // tokens that stay in any case are counted apart: they are many of one key
-  int always = 0;
-  each([&](int, uint32_t k) __attribute__((always_inline)) {
-    always += __popcll(ballot(k == kStays));
-    add_to_bins(sh.hist, k != 0u && k != kStays, k >> (32 - kDigit), lane);
-  });
-  if (lane == 0) sh.count[0][wave] = always;
-  __syncthreads();
-  always = 0;
+  // The key of the keep-th greatest, and how many of those equal to it stay: by 11
+  // bits at a time, among the keys that have tau's bits above them.
+  uint32_t tau = 0u, above = 0u, rank = (uint32_t)keep, ties;
+  for (int down = 32 - kDigit;;) {
+    each([&](int, const uint32_t* k) __attribute__((always_inline)) {
+      uint32_t bin[4];
+      bool in[4];
 #pragma unroll
-  for (int v = 0; v < W; ++v) always += sh.count[0][v];
-  // keys above t_sure stay, and the first `need` of those equal to it + 1
-  uint32_t t_sure;
-  int need = 0;
-  if (always >= keep) {
-    t_sure = kStays - 1u;
-    need = keep < always ? keep : 0;
-  } else {
-    uint32_t prefix = 0u, rank = (uint32_t)(keep - always);
-    int shift = 32 - kDigit;
-    for (;;) {
-      find_bin<W>(sh, rank);
-      prefix |= sh.found[0] << shift;
-      rank = sh.found[1];
-      const bool all = rank == sh.found[2];  // every key of the bin stays
-      if (all || shift == 0) {
-        t_sure = prefix - 1u;
-        need = all ? 0 : (int)rank;
-        break;
+      for (int e = 0; e < 4; ++e) {
+        in[e] = ((k[e] ^ tau) & above) == 0u;
+        bin[e] = (k[e] >> down) & (kBins - 1);
       }
-      const int up = shift, down = max(shift - kDigit, 0);
-      each([&](int, uint32_t k) __attribute__((always_inline)) {
-        add_to_bins(sh.hist, (k ^ prefix) >> up == 0u && k != kStays, (k & ((1u << up) - 1u)) >> down, lane);
+      const uint64_t act = ballot(in[0]);
+      // Many lanes of one bin (equal weights, tokens that stay in any case, none
+      // at all) are added as one: atomics on one word run one after another.
+      bool clustered = false;
+      if (act != 0ull) {
+        const uint32_t lead = (uint32_t)__builtin_amdgcn_readlane((int)bin[0], __builtin_ctzll(act));
+        clustered = __popcll(ballot(in[0] && bin[0] == lead)) >= 16;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        bool add = in[e];
+        if (clustered) {  // uniform
+          const uint64_t on = ballot(add);
+          if (on == 0ull) continue;
+          const int lead = __builtin_ctzll(on);
+          const uint64_t same = ballot(add && bin[e] == (uint32_t)__builtin_amdgcn_readlane((int)bin[e], lead));
+          if (lane == lead) atomicAdd(&sh.hist[bin[e]], (uint32_t)__popcll(same));
+          add = add && !(same >> lane & 1ull);
+        }
+        if (add) atomicAdd(&sh.hist[bin[e]], 1u);
+      }
+    });
+    __syncthreads();
+    find_bin<W>(sh, rank);
+    tau |= (uint32_t)uniform((int)sh.found[0]) << down;
+    rank = (uint32_t)uniform((int)sh.found[1]);
+    ties = (uint32_t)uniform((int)sh.found[2]);
+    above = ~((1u << down) - 1u);
+    if (down == 0 || rank == ties) break;  // one key, or every key of the bin stays
+    if (ties <= kList) {  // its keys, in any order, compared with each other
+      each([&](int, const uint32_t* k) __attribute__((always_inline)) {
+        uint32_t d[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) d[e] = (k[e] ^ tau) & above;
+        if (min(min(d[0], d[1]), min(d[2], d[3])) == 0u) {  // few lanes hold one
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (d[e] == 0u) sh.list[atomicAdd(&sh.listed, 1u)] = k[e];
+        }
       });
-      shift = down;
       __syncthreads();
+      const int m = (int)ties;
+      if (tid < m) {
+        const uint32_t mine = sh.list[tid];
+        uint32_t gt = 0u, ge = 0u;
+        for (int i = 0; i < m; ++i) {
+          const uint32_t o = sh.list[i];
+          gt += o > mine;
+          ge += o >= mine;
+        }
+        if (gt < rank && rank <= ge) {  // equal keys write the same
+          sh.found[0] = mine;
+          sh.found[1] = rank - gt;
+          sh.found[2] = ge - gt;
+        }
+      }
+      __syncthreads();
+      tau = (uint32_t)uniform((int)sh.found[0]);
+      rank = (uint32_t)uniform((int)sh.found[1]);
+      ties = (uint32_t)uniform((int)sh.found[2]);
+      break;
     }
+    down = max(down - kDigit, 0);
   }
-  const bool all_ties = need == 0;  // ties: keys equal to t_sure + 1, if they do not all stay
-  int tie0 = 0;
-  if (!all_ties) {
-    int ties = 0;
-    each([&](int, uint32_t k) __attribute__((always_inline)) { ties += __popcll(ballot(k == t_sure + 1u)); });
-    if (lane == 0) sh.count[2][wave] = ties;
+  // keys above t_sure stay; of those equal to tau the first `need`, or (need 0) all
+  const uint32_t t_sure = rank == ties ? tau - 1u : tau;
+  const uint32_t need = rank == ties ? 0u : rank;
+  uint32_t tie0 = 0u;  // ties in the rows before this wave's
+  if (need > 0u) {
+    int here = 0;
+    each([&](int, const uint32_t* k) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) here += __popcll(ballot(k[e] == tau));
+    });
+    if (lane == 0) sh.count[2][wave] = here;
     __syncthreads();
 #pragma unroll
-    for (int v = 0; v < W; ++v) tie0 += v < wave ? sh.count[2][v] : 0;
+    for (int v = 0; v < W; ++v) tie0 += v < wave ? (uint32_t)sh.count[2][v] : 0u;
   }
-  // f(first row of 64, rows to be freed, rows that move) of this wave
-  auto moves_of = [&](auto&& f) __attribute__((always_inline)) {
-    int before = tie0;
-    each([&](int b, uint32_t k) __attribute__((always_inline)) {
-      uint64_t stay;
-      if (all_ties) {  // uniform
-        stay = ballot(k > t_sure);
-      } else {
-        const uint64_t ties = ballot(k == t_sure + 1u);
-        stay = ballot(k > t_sure + 1u || (k == t_sure + 1u && before + lanes_below(ties) < need));
-        before += __popcll(ties);
+  // f(first row of the group, which of this lane's four stay) over this wave's rows
+  auto stays_of = [&](auto&& f) __attribute__((always_inline)) {
+    uint32_t before = tie0;
+    each([&](int j, const uint32_t* k) __attribute__((always_inline)) {
+      bool stay[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) stay[e] = k[e] > t_sure;
+      if (need > 0u) {  // uniform
+        uint64_t eq[4];
+        uint32_t mine = before;  // ties before this lane's
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          eq[e] = ballot(k[e] == tau);
+          mine += (uint32_t)lanes_below(eq[e]);
+          before += (uint32_t)__popcll(eq[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool tie = k[e] == tau;
+          stay[e] = stay[e] || (tie && mine < need);
+          mine += tie ? 1u : 0u;
+        }
       }
-      const int j = j0 + b * kWave;
-      if (b >= nb) return;  // uniform: a batch may end past the wave's rows
-      const uint64_t low = keep - j >= kWave ? ~0ull : (keep > j ? (1ull << (keep - j)) - 1ull : 0ull);
-      f(j, ~stay & low, stay & ~low);
+      f(j, stay);
     });
   };
   int frees = 0, goes = 0;
-  moves_of([&](int, uint64_t free, uint64_t go) __attribute__((always_inline)) {
-    frees += __popcll(free);
-    goes += __popcll(go);
+  stays_of([&](int j, const bool* stay) __attribute__((always_inline)) {
+    int n_stay = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) n_stay += __popcll(ballot(stay[e]));
+    int df = j + kGroup <= keep ? kGroup - n_stay : 0, dg = j >= keep ? n_stay : 0;
+    if (j < keep && j + kGroup > keep) {  // uniform: both
+      df = dg = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool low = j + 4 * lane + e < keep;
+        df += __popcll(ballot(low && !stay[e]));
+        dg += __popcll(ballot(!low && stay[e]));
+      }
+    }
+    frees += df;
+    goes += dg;
   });
-  __syncthreads();  // sh.count is read above
   if (lane == 0) {
     sh.count[0][wave] = frees;
     sh.count[1][wave] = goes;
@@ -249,20 +313,42 @@ __global__ __launch_bounds__(W * kWave) void evict8_kernel(Evict8Args a) {
     gb += v < wave ? sh.count[1][v] : 0;
     all += sh.count[1][v];
   }
-  // the moves: the i-th row to be freed and the i-th token that moves
+  // The moves: the i-th row to be freed and the i-th token that moves. Rows of one
+  // group below `keep` (tokens that leave are listed) or not (those that stay are).
   int2* const moves = a.moves + (size_t)lh * (c.rows / 2) + row0 / 2;
+  char* const list = reinterpret_cast<char*>(moves);
+  auto emit = [&](int j, const bool* on, int& base, uint32_t half) __attribute__((always_inline)) {
+    int mine = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mine += on[e];
+    if (ballot(mine > 0) == 0ull) return;
+    const int incl = wave_scan(mine);
+    // 32-bit byte offsets: there are less than 2^29 moves
+    uint32_t at = 8u * (uint32_t)(base + incl - mine) + half;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (on[e]) {
+        *reinterpret_cast<int*>(list + at) = j + 4 * lane + e;
+        at += 8u;
+      }
+    }
+    base += wave_total(incl);
+  };
   if (frees + goes > 0)  // uniform over the wave
-    moves_of([&](int j, uint64_t free, uint64_t go) __attribute__((always_inline)) {
-      if ((free | go) == 0ull) return;
-      if (free >> lane & 1ull) moves[fb + lanes_below(free)].x = j + lane;
-      if (go >> lane & 1ull) moves[gb + lanes_below(go)].y = j + lane;
-      fb += __popcll(free);
-      gb += __popcll(go);
+    stays_of([&](int j, const bool* stay) __attribute__((always_inline)) {
+      bool on[4];
+      if (j < keep) {  // uniform
+#pragma unroll
+        for (int e = 0; e < 4; ++e) on[e] = j + 4 * lane + e < keep && !stay[e];
+        emit(j, on, fb, 0u);
+      }
+      if (j + kGroup > keep) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) on[e] = j + 4 * lane + e >= keep && stay[e];
+        emit(j, on, gb, 4u);
+      }
     });
-  if (tid == 0) {
-    const size_t sc = (size_t)lh * c.nblk + first_block(row0, s) + keep / kBlock8;
-    *head = Evict8Head{all, keep, c.k_scales[sc], c.v_scales[sc]};
-  }
+  if (tid == 0) *head = Evict8Head{all, keep, k_edge, v_edge};
 }
 
 // The exponent that e4m3 codes with these largest magnitude bits need, as
@@ -478,11 +564,13 @@ hipError_t launch_evict8(const Evict8Args& a, hipStream_t st) {
   };
   using std::integral_constant;
   const integral_constant<bool, false> once{};
-  if (a.longest <= 4 * 64 * 8) run(integral_constant<int, 4>{}, integral_constant<int, 8>{}, once);
-  else if (a.longest <= 4 * 64 * 40) run(integral_constant<int, 4>{}, integral_constant<int, 40>{}, once);
-  else if (a.longest <= 16 * 64 * 32) run(integral_constant<int, 16>{}, integral_constant<int, 32>{}, once);
-  else if (a.longest <= 16 * 64 * 80) run(integral_constant<int, 16>{}, integral_constant<int, 80>{}, once);
-  else run(integral_constant<int, 16>{}, integral_constant<int, 16>{}, integral_constant<bool, true>{});
+  const integral_constant<int, 4> four{};
+  const integral_constant<int, 16> sixteen{};
+  if (a.longest <= 4 * 256 * 2) run(four, integral_constant<int, 2>{}, once);
+  else if (a.longest <= 4 * 256 * 10) run(four, integral_constant<int, 10>{}, once);
+  else if (a.longest <= 16 * 256 * 8) run(sixteen, integral_constant<int, 8>{}, once);
+  else if (a.longest <= 16 * 256 * 20) run(sixteen, integral_constant<int, 20>{}, once);
+  else run(sixteen, integral_constant<int, 4>{}, integral_constant<bool, true>{});
   const dim3 grid((unsigned)move_workgroups(a));
   if (a.c.d == 128)
     hipLaunchKernelGGL(move8_kernel<128>, grid, dim3(kMoveThreads), 0, st, a);
