@@ -105,9 +105,11 @@ size_t decode_bytes(const Attend8Args& a, bool gather) {
   return partial_bytes(a) + (gather ? logits_bytes(a) + norms_bytes(a) : 0);
 }
 
-Evict8Args evict_args(const stepkv_cache8* c) {
+Evict8Args evict_args(const stepkv_cache8* c, int32_t keep, const int32_t* keeps) {
   Evict8Args a{};
   a.c = view(c);
+  a.keep = keep;
+  a.keeps = keeps;
   plan_evict8(a, c->cu_rows_host);
   return a;
 }
@@ -254,7 +256,7 @@ int stepkv_cache8_decode(const stepkv_cache8* c, int32_t num_q_heads, const void
 
 size_t stepkv_cache8_evict_workspace_bytes(const stepkv_cache8* c) {
   if (check_cache(c) != STEPKV_OK) return 0;
-  return evict_bytes(evict_args(c));
+  return evict_bytes(evict_args(c, 1, nullptr));
 }
 
 int stepkv_cache8_evict(const stepkv_cache8* c, int32_t keep, const int32_t* keeps, int32_t first,
@@ -262,12 +264,10 @@ int stepkv_cache8_evict(const stepkv_cache8* c, int32_t keep, const int32_t* kee
   const int rc = check_cache(c);
   if (rc != STEPKV_OK) return rc;
   if (!gathers(c) || first < 0 || recent < 0 || (!keeps && keep < 1)) return STEPKV_EINVAL;
-  Evict8Args a = evict_args(c);
+  Evict8Args a = evict_args(c, keep, keeps);
   if (!evict8_fits(a)) return STEPKV_EUNSUPPORTED;
   if (!workspace || !aligned(workspace, kAlign) || ws_bytes < evict_bytes(a))
     return STEPKV_EWORKSPACE;
-  a.keeps = keeps;
-  a.keep = keep;
   a.first = first;
   a.recent = recent;
   a.heads = static_cast<Evict8Head*>(workspace);

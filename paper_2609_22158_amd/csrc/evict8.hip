@@ -399,7 +399,8 @@ __device__ __forceinline__ uint32_t top_of16(u32x4_t w) {
 template <int D>
 __global__ __launch_bounds__(kMoveThreads) void move8_kernel(Evict8Args a) {
   constexpr int PR = D / 16;      // pieces of a row
-  constexpr int RP = kWave / PR;  // rows at a time
+  constexpr int RP = kWave / PR;  // rows of a load
+  constexpr int kRows = 16 / RP > 0 ? 16 / RP : 1;  // loads in flight, of each tensor
   const Cache8View& c = a.c;
   const int lane = threadIdx.x & 63;
   const int64_t worker = (int64_t)blockIdx.x * (kMoveThreads / kWave) + uniform(threadIdx.x >> 6);
@@ -420,117 +421,142 @@ __global__ __launch_bounds__(kMoveThreads) void move8_kernel(Evict8Args a) {
     // moves lo .. end - 1: from the first that begins a block at or past the chunk's
     // start to the last of the block that its last move is into
     const int c0 = (int)(chunk * kMoveChunk), c1 = min(c0 + kMoveChunk, head.moves);
-    const int prev = c0 > 0 ? moves[c0 - 1].x / kBlock8 : -1;
-    const int last = moves[c1 - 1].x / kBlock8;
-    if (prev == last) continue;  // all of them another chunk's
-    // a block has 64 rows at most, and the chunk begins within one and ends within one
-    for (int i = c0; i < head.moves;) {  // lanes: moves i .. i + 63
+    const int before = moves[max(c0 - 1, 0)].x / kBlock8, last = moves[c1 - 1].x / kBlock8;
+    const int prev = c0 > 0 ? before : -1;
+    for (int i = c0;;) {  // lanes: moves i .. i + 63
       int2 m = make_int2(-1, -1);
       if (i + lane < head.moves) m = moves[i + lane];
+      if (prev == last) break;  // all of them another chunk's
       const int b = m.x < 0 ? -1 : m.x / kBlock8;
-      // of these, those into the chunk's blocks whose last move is among them too
-      // (the block of the 64th may go on: it is taken up again from its first move)
-      const int b63 = __builtin_amdgcn_readlane(b, kWave - 1);
-      const int b0 = __builtin_amdgcn_readfirstlane(b);
-      const bool whole = b63 < 0 || b63 != b || i + kWave >= head.moves || b63 == b0;
-      const bool mine = b > prev && b <= last && b >= 0 && whole;
+      // of these, the moves into the chunk's blocks, but for a block that goes on after
+      // the 64th (it is taken up again from its first move; no block has more than 64)
+      const int b0 = uniform(b), b63 = __builtin_amdgcn_readlane(b, kWave - 1);
+      const bool mine = b > prev && b <= last && (b != b63 || b63 == b0 || i + kWave >= head.moves);
       const uint64_t mask = ballot(mine);
-      const uint64_t passed = ballot(b >= 0 && (b <= prev || mine));  // these and what is before them
-      const int step = __popcll(passed);
-      if (mask == 0ull) {
-        if (step == 0) break;
-        i += step;
-        continue;
-      }
-      const int i0 = __builtin_ctzll(mask), count = __popcll(mask);  // consecutive lanes
-      // scales as they were: of the blocks moved into, and of those moved out of
-      float kd = 1.f, vd = 1.f, ks = 1.f, vs = 1.f;
-      if (mine) {
-        kd = c.k_scales[scales + b];
-        vd = c.v_scales[scales + b];
-        const int f = m.y / kBlock8;
-        ks = f == edge ? head.k_scale : c.k_scales[scales + f];
-        vs = f == edge ? head.v_scale : c.v_scales[scales + f];
-      }
-      // what the rows need, and whether a block's scale is less
-      int ek = kLeast8, ev = kLeast8;
-      for (int j0 = 0; j0 < count; j0 += RP) {
-        const int j = i0 + min(j0 + sub, count - 1);
-        const int from = __shfl(m.y, j, kWave);
-        uint32_t kt = top_of16(reinterpret_cast<const u32x4_t*>(c.k_codes + (base + from) * D)[piece]);
-        uint32_t vt = top_of16(reinterpret_cast<const u32x4_t*>(c.v_codes + (base + from) * D)[piece]);
+      const int step = __popcll(ballot(b >= 0 && (b <= prev || mine)));  // the first `step` lanes are done with
+      if (mask != 0ull) {
+        const int i0 = __builtin_ctzll(mask), count = __popcll(mask);  // consecutive lanes
+        u32x4_t kw[kRows], vw[kRows];  // 16 bytes of kRows rows, of the moves from i0 + j0 on
+        auto load_rows = [&](int j0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int off = PR / 2; off > 0; off >>= 1) {
-          kt = max(kt, (uint32_t)__shfl_xor((int)kt, off, kWave));
-          vt = max(vt, (uint32_t)__shfl_xor((int)vt, off, kWave));
+          for (int u = 0; u < kRows; ++u) {
+            const int from = __shfl(m.y, i0 + min(j0 + u * RP + sub, count - 1), kWave);
+            kw[u] = reinterpret_cast<const u32x4_t*>(c.k_codes + (base + from) * D)[piece];
+            vw[u] = reinterpret_cast<const u32x4_t*>(c.v_codes + (base + from) * D)[piece];
+          }
+        };
+        load_rows(0);
+        // what moves along, and scales as they were: of the blocks moved into, and of
+        // those moved out of
+        float kd = 1.f, vd = 1.f, ks = 1.f, vs = 1.f, weight = 0.f;
+        int position = 0;
+        if (mine) {
+          const int f = m.y / kBlock8;
+          kd = c.k_scales[scales + b];
+          vd = c.v_scales[scales + b];
+          ks = c.k_scales[scales + f];
+          vs = c.v_scales[scales + f];
+          weight = c.weights[base + m.y];
+          position = c.positions[base + m.y];
+          if (f == edge) ks = head.k_scale, vs = head.v_scale;
         }
-        // to the lane of the move: its row is the (lane - i0 - j0)-th of these
-        const int back = (lane - i0 - j0) * PR;
-        const uint32_t kb = (uint32_t)__shfl((int)kt, back & 63, kWave);
-        const uint32_t vb = (uint32_t)__shfl((int)vt, back & 63, kWave);
-        if (back >= 0 && back < kWave && mine) {
-          ek = need_of_code(kb, exponent_of(ks));
-          ev = need_of_code(vb, exponent_of(vs));
-        }
-      }
-      const bool grows = mine && (ek > exponent_of(kd) || ev > exponent_of(vd));
-      for (uint64_t left = ballot(grows); left != 0ull;) {  // blocks that grow: rare
-        const int lead = __builtin_ctzll(left);
-        const int gbk = __builtin_amdgcn_readlane(b, lead);
-        const bool here = mine && b == gbk;
-        left &= ~ballot(here);
-        int nk = here ? ek : kLeast8, nv = here ? ev : kLeast8;
-        uint64_t taken = here ? 1ull << (m.x % kBlock8) : 0ull;  // rows that are replaced
+        // what the rows need, and whether a block's scale is less
+        int ek = kLeast8, ev = kLeast8;
+        auto look = [&](int j0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int off = 32; off > 0; off >>= 1) {
-          nk = max(nk, __shfl_xor(nk, off, kWave));
-          nv = max(nv, __shfl_xor(nv, off, kWave));
-          taken |= (uint64_t)__shfl_xor((unsigned long long)taken, off, kWave);
-        }
-        const float k_old = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(kd), lead));
-        const float v_old = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(vd), lead));
-        const int ok = uniform(exponent_of(k_old)), ov = uniform(exponent_of(v_old));
-        nk = uniform(min(max(nk, ok), kMost8));
-        nv = uniform(min(max(nv, ov), kMost8));
-        const float kn = nk > ok ? pow2_of(nk) : k_old, vn = nv > ov ? pow2_of(nv) : v_old;
-        for (int j0 = 0; j0 < kBlock8; j0 += RP) {  // the block's other tokens
-          const int j = j0 + sub;
-          if (gbk * kBlock8 + j >= head.keep || (taken >> j & 1ull)) continue;
-          const size_t r = base + (size_t)gbk * kBlock8 + j;
-          if (nk > ok) {
-            u32x4_t* p = reinterpret_cast<u32x4_t*>(c.k_codes + r * D) + piece;
-            *p = regrid16(*p, k_old, kn);
+          for (int u = 0; u < kRows; ++u) {
+            uint32_t kt = top_of16(kw[u]), vt = top_of16(vw[u]);
+#pragma unroll
+            for (int off = PR / 2; off > 0; off >>= 1) {
+              kt = max(kt, (uint32_t)__shfl_xor((int)kt, off, kWave));
+              vt = max(vt, (uint32_t)__shfl_xor((int)vt, off, kWave));
+            }
+            // to the lane of the move: its row is the (lane - i0 - j0 - u RP)-th of these
+            const int back = (lane - i0 - j0 - u * RP) * PR;
+            const uint32_t kb = (uint32_t)__shfl((int)kt, back & 63, kWave);
+            const uint32_t vb = (uint32_t)__shfl((int)vt, back & 63, kWave);
+            if (back >= 0 && back < kWave && mine) {
+              ek = need_of_code(kb, exponent_of(ks));
+              ev = need_of_code(vb, exponent_of(vs));
+            }
           }
-          if (nv > ov) {
-            u32x4_t* p = reinterpret_cast<u32x4_t*>(c.v_codes + r * D) + piece;
-            *p = regrid16(*p, v_old, vn);
+        };
+        look(0);
+        for (int j0 = kRows * RP; j0 < count; j0 += kRows * RP) {
+          load_rows(j0);
+          look(j0);
+        }
+        const bool grows = mine && (ek > exponent_of(kd) || ev > exponent_of(vd));
+        for (uint64_t left = ballot(grows); left != 0ull;) {  // blocks that grow: rare
+          const int lead = __builtin_ctzll(left);
+          const int at_b = __builtin_amdgcn_readlane(b, lead);
+          const bool here = mine && b == at_b;
+          left &= ~ballot(here);
+          int nk = here ? ek : kLeast8, nv = here ? ev : kLeast8;
+          uint64_t taken = here ? 1ull << (m.x % kBlock8) : 0ull;  // rows that are replaced
+#pragma unroll
+          for (int off = 32; off > 0; off >>= 1) {
+            nk = max(nk, __shfl_xor(nk, off, kWave));
+            nv = max(nv, __shfl_xor(nv, off, kWave));
+            taken |= (uint64_t)__shfl_xor((unsigned long long)taken, off, kWave);
+          }
+          const float k_old = __shfl(kd, lead, kWave), v_old = __shfl(vd, lead, kWave);
+          const int ok = uniform(exponent_of(k_old)), ov = uniform(exponent_of(v_old));
+          nk = uniform(min(max(nk, ok), kMost8));
+          nv = uniform(min(max(nv, ov), kMost8));
+          const float kn = nk > ok ? pow2_of(nk) : k_old, vn = nv > ov ? pow2_of(nv) : v_old;
+#pragma nounroll
+          for (int j0 = 0; j0 < kBlock8; j0 += RP) {  // the block's other tokens
+            const int j = j0 + sub;
+            if (at_b * kBlock8 + j >= head.keep || (taken >> j & 1ull)) continue;
+            const size_t r = base + (size_t)at_b * kBlock8 + j;
+            if (nk > ok) {
+              u32x4_t* p = reinterpret_cast<u32x4_t*>(c.k_codes + r * D) + piece;
+              *p = regrid16(*p, k_old, kn);
+            }
+            if (nv > ov) {
+              u32x4_t* p = reinterpret_cast<u32x4_t*>(c.v_codes + r * D) + piece;
+              *p = regrid16(*p, v_old, vn);
+            }
+          }
+          if (lane == lead) {
+            c.k_scales[scales + at_b] = kn;
+            c.v_scales[scales + at_b] = vn;
+          }
+          if (here) {
+            kd = kn;
+            vd = vn;
           }
         }
-        if (lane == lead) {
-          c.k_scales[scales + gbk] = kn;
-          c.v_scales[scales + gbk] = vn;
+        auto store_rows = [&](int j0) __attribute__((always_inline)) {
+#pragma unroll
+          for (int u = 0; u < kRows; ++u) {
+            const int at_j = j0 + u * RP + sub, j = i0 + min(at_j, count - 1);
+            const int to = __shfl(m.x, j, kWave);
+            const float fk = __shfl(ks, j, kWave), fv = __shfl(vs, j, kWave);
+            const float tk = __shfl(kd, j, kWave), tv = __shfl(vd, j, kWave);
+            if (at_j < count) {
+              reinterpret_cast<u32x4_t*>(c.k_codes + (base + to) * D)[piece] = regrid16(kw[u], fk, tk);
+              reinterpret_cast<u32x4_t*>(c.v_codes + (base + to) * D)[piece] = regrid16(vw[u], fv, tv);
+            }
+          }
+        };
+        if (count <= kRows * RP) {  // the rows are still there
+          store_rows(0);
+        } else {
+          for (int j0 = 0; j0 < count; j0 += kRows * RP) {
+            load_rows(j0);
+            store_rows(j0);
+          }
         }
-        if (here) {
-          kd = kn;
-          vd = vn;
+        if (mine) {
+          c.weights[base + m.x] = weight;
+          c.positions[base + m.x] = position;
         }
       }
-      for (int j0 = 0; j0 < count; j0 += RP) {
-        const int j = i0 + min(j0 + sub, count - 1);
-        const int from = __shfl(m.y, j, kWave), to = __shfl(m.x, j, kWave);
-        const float fk = __shfl(ks, j, kWave), fv = __shfl(vs, j, kWave);
-        const float tk = __shfl(kd, j, kWave), tv = __shfl(vd, j, kWave);
-        if (j0 + sub >= count) continue;
-        const u32x4_t kw = reinterpret_cast<const u32x4_t*>(c.k_codes + (base + from) * D)[piece];
-        const u32x4_t vw = reinterpret_cast<const u32x4_t*>(c.v_codes + (base + from) * D)[piece];
-        reinterpret_cast<u32x4_t*>(c.k_codes + (base + to) * D)[piece] = regrid16(kw, fk, tk);
-        reinterpret_cast<u32x4_t*>(c.v_codes + (base + to) * D)[piece] = regrid16(vw, fv, tv);
-      }
-      if (mine) {
-        c.weights[base + m.x] = c.weights[base + m.y];
-        c.positions[base + m.x] = c.positions[base + m.y];
-      }
+      if (step == 0 || b63 < 0 || b63 > last) break;  // the chunk's last move is among these
       i += step;
+      if (i >= head.moves) break;
     }
   }
 }
@@ -542,13 +568,15 @@ int64_t move_workgroups(const Evict8Args& a) {
 }  // namespace
 
 // Waves that move rows: as many as the chip holds, but no more than there can be
-// chunks of moves.
+// chunks of moves (with keeps on the device, half as many: most find none).
 void plan_evict8(Evict8Args& a, const int32_t* cu_rows_host) {
   a.longest = 0;
   for (int s = 0; s < a.c.S; ++s) a.longest = std::max(a.longest, cu_rows_host[s + 1] - cu_rows_host[s]);
-  const int64_t heads = (int64_t)a.c.L * a.c.H * a.c.S;
+  const int64_t heads = (int64_t)a.c.L * a.c.H * a.c.S, want = a.keeps ? 4096 : 8192;
+  int64_t most = a.longest / 2;
+  if (!a.keeps) most = std::min<int64_t>(most, std::max(a.longest - a.keep, 1));
   a.workers = (int)std::max<int64_t>(
-      1, std::min<int64_t>((8192 + heads - 1) / heads, (a.longest / 2 + kMoveChunk - 1) / kMoveChunk));
+      1, std::min<int64_t>((want + heads - 1) / heads, (most + kMoveChunk - 1) / kMoveChunk));
 }
 
 bool evict8_fits(const Evict8Args& a) {
