@@ -22,9 +22,8 @@
 //    that are it exactly (in one operand for narrow groups); the same parts times
 //    ones give the softmax's sum.
 // combine8_kernel merges the splits. To gather weights the logits are kept (4
-// bytes a query head and token, 2 to 12 % of the cache's), and gather8_kernel, or
-// the workgroup that has the whole sequence, turns them into weights once the
-// row's maximum and sum are known.
+// bytes a query head and token), and the same launch, or the workgroup that has the
+// whole sequence, turns them into weights once the row's maximum and sum are known.
 #include "cache8_device.h"
 
 #include <math.h>
@@ -41,7 +40,7 @@ typedef __attribute__((address_space(3))) i32x2_t lds_i32x2;
 constexpr int kTile = 32;  // tokens a wave computes at a time
 constexpr int kWaves = 4;  // waves of a workgroup
 constexpr int kMergeThreads = 256;  // of a merge of many rows
-constexpr int kGatherThreads = 256;
+constexpr int kMergeOne = 512;      // and of a merge of one query head
 constexpr float kSlack = 16.f;
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -84,9 +83,7 @@ constexpr float kNoWeight = -3.40282347e38f;
 __device__ __forceinline__ void finish(const Attend8Args& a, size_t row, int ch, int D, float M,
                                        float Z, float O) {
   a.out[row * D + ch] = M == -INFINITY && Z == 0.f ? 0.f : O / Z;
-  if (ch != 0) return;
-  if (a.lse) a.lse[row] = Z == 0.f ? -INFINITY : (M + log2f(Z)) * 0.693147180559945309f;
-  if (a.logits && !a.single) a.norms[row] = make_float2(M, 1.f / Z);
+  if (a.lse && ch == 0) a.lse[row] = Z == 0.f ? -INFINITY : (M + log2f(Z)) * 0.693147180559945309f;
 }
 
 // The logits are kept by tiles of 32 tokens, [L*H*tiles][rows / 32 + S][min(G, 16)][32]:
@@ -339,15 +336,10 @@ void attend8_kernel(Attend8Args a) {
     }
   }
   if constexpr (GATHER) {
-    // The whole sequence's logits, by this workgroup's waves: the weights, unless
-    // other workgroups have other heads of the same KV head.
+    // All heads' logits of the whole sequence are this workgroup's: their weights.
     if (!a.single) return;
     __threadfence_block();
     __syncthreads();
-    if (tiles > 1) {
-      if (tid < heads) a.norms[row_out + tid] = norm_s[tid];
-      return;
-    }
     const float* __restrict__ base = a.logits + logits_at(a, unit, seq_row, s);
     for (int j = tid; j < held; j += NW * kWave) {
       float w = 0.f;
@@ -359,35 +351,113 @@ void attend8_kernel(Attend8Args a) {
   }
 }
 
+// The splits of sequence s in the partial states of a unit: its first, and how many.
+__device__ __forceinline__ void splits_of(const Attend8Args& a, int s, int& first, int& n) {
+  const int lane = threadIdx.x & 63;
+  const int split = rows_per_split(a);
+  first = 0;
+  for (int s0 = 0; s0 < s; s0 += kWave)
+    first += wave_total(
+        wave_scan(s0 + lane < s ? (held_tokens(a.c, s0 + lane) + split - 1) / split : 0));
+  first = min(first, a.splits);
+  n = min((held_const(a.c, s) + split - 1) / split, a.splits - first);
+}
+
+// weights += the weights of THREADS * 4 tokens of a (layer, KV head, sequence), four
+// a thread: the sum over the group's heads in their order. A wave finds what a head's
+// softmax is taken over from the states of the splits.
+template <int D, int THREADS>
+__device__ __forceinline__ void gather(const Attend8Args& a, int at) {
+  constexpr int ST = D + 2;
+  constexpr int kRows = 4 * THREADS;
+  __shared__ float2 norm_s[16];
+  const Cache8View& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int per = c.rows / kRows + c.S;  // chunks that a (layer, KV head) may have
+  const int lh = uniform(at / per);
+  at -= lh * per;
+  int s = 0, first = 0;
+  locate_item(c.S, at, [&](int sq) { return (held_tokens(c, sq) + kRows - 1) / kRows; }, s, first);
+  if (s < 0) return;
+  s = uniform(s);
+  const int j = (at - first) * kRows + 4 * tid, held = held_const(c, s);
+  int split0, splits;
+  splits_of(a, s, split0, splits);
+  const int seq_row = read_const(c.cu_rows, s), tiles = (a.G + 15) / 16, wide = min(a.G, 16);
+  const float cl2 = a.scale * kLog2e;
+  float* const to = c.weights + (size_t)lh * c.rows + seq_row + j;
+  float w[4] = {}, was[4];
+  if (j + 4 <= held) __builtin_memcpy(was, to, 16);
+  for (int t = 0; t < tiles; ++t) {
+    const int unit = lh * tiles + t, heads = min(a.G - 16 * t, 16);
+    const float* __restrict__ part = a.partial + ((size_t)unit * a.splits + split0) * wide * ST;
+    if (t > 0) __syncthreads();  // norm_s is read
+    for (int g = wave; g < heads; g += THREADS / kWave) {
+      float M = -INFINITY, Z = 0.f;
+      for (int i = lane; i < splits; i += kWave) {
+        const float* __restrict__ p = part + ((size_t)i * wide + g) * ST + D;
+        const float m = p[0], z = p[1], top = fmaxf(M, m);
+        Z = (M == -INFINITY ? 0.f : Z * fast_exp2(M - top)) + (m == -INFINITY ? 0.f : z * fast_exp2(m - top));
+        M = top;
+      }
+      const float top = wave_max(M);
+      const float sum = wave_sum(M == -INFINITY ? 0.f : Z * fast_exp2(M - top));
+      if (lane == 0) norm_s[g] = make_float2(top, 1.f / sum);
+    }
+    __syncthreads();
+    if (j >= held) continue;
+    const float* __restrict__ z = a.logits + logits_at(a, unit, seq_row, s) + token_at(a, j);
+#pragma unroll 4
+    for (int g = 0; g < heads; ++g) {
+      const f32x4_t y = *reinterpret_cast<const f32x4_t*>(z + g * kTile);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] += weight_of(y[e], cl2, norm_s[g]);
+    }
+  }
+  if (j + 4 <= held) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) was[e] += w[e];
+    __builtin_memcpy(to, was, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (j + e < held) to[e] += w[e];
+  }
+}
+
 // out and lse of a (layer, sequence, KV head, 16 query heads), or of one query
 // head of them: the splits' states merged by a running maximum, four in flight
 // per thread. A thread per (head, channel), or with one head a group of
-// THREADS / D threads per channel over the splits, merged in order.
-template <int D, int THREADS, bool ONE>
-__global__ __launch_bounds__(THREADS) void combine8_kernel(Attend8Args a) {
+// THREADS / D threads per channel over the splits, merged in order. With GATHER the
+// first `gathers` workgroups add up weights instead.
+template <int D, int THREADS, bool ONE, bool GATHER>
+__global__ __launch_bounds__(THREADS) void combine8_kernel(Attend8Args a, int gathers) {
   constexpr int ST = D + 2;
   constexpr int J = ONE ? THREADS / D : 1;
   constexpr int kAhead = 4;
   __shared__ float om[J][D], mm[J], zm[J];
   const Cache8View& c = a.c;
-  const int tid = threadIdx.x, lane = tid & 63;
+  int at = blockIdx.x;
+  if constexpr (GATHER) {
+    if (at < gathers) {
+      gather<D, THREADS>(a, at);
+      return;
+    }
+    at -= gathers;
+  }
+  const int tid = threadIdx.x;
   const int tiles = (a.G + 15) / 16, per = min(a.G, 16);
-  int at = blockIdx.x, g0 = 0;
+  int g0 = 0;
   if (ONE) {
     g0 = uniform(at % per);
     at = uniform(at / per);
   }
-  const int unit = uniform(at / c.S), s = at - unit * c.S;
+  const int unit = uniform(at / c.S), s = uniform(at - unit * c.S);
   const int lh = unit / tiles, hd0 = 16 * (unit - lh * tiles) + g0;
   const int heads = ONE ? 1 : min(a.G - hd0, 16);
   if (hd0 >= a.G) return;  // the last tile may be narrower: uniform
-  const int split = rows_per_split(a);
-  int first = 0;  // splits of the sequences before s
-  for (int s0 = 0; s0 < s; s0 += kWave)
-    first += wave_total(
-        wave_scan(s0 + lane < s ? (held_tokens(c, s0 + lane) + split - 1) / split : 0));
-  first = min(first, a.splits);
-  const int n = min((held_const(c, s) + split - 1) / split, a.splits - first);
+  int first, n;
+  splits_of(a, s, first, n);
   const size_t stride = (size_t)per * ST;
   const float* __restrict__ base =
       a.partial + ((size_t)unit * a.splits + first) * stride + (size_t)g0 * ST;
@@ -450,36 +520,11 @@ __global__ __launch_bounds__(THREADS) void combine8_kernel(Attend8Args a) {
   }
 }
 
-// weights += the tokens' weights, a thread per token: the sum over the group's
-// heads in their order.
-__global__ __launch_bounds__(kGatherThreads) void gather8_kernel(Attend8Args a) {
-  const Cache8View& c = a.c;
-  const int per = c.rows / kGatherThreads + c.S;  // chunks that a (layer, KV head) may have
-  const int lh = uniform(blockIdx.x / per), at = uniform(blockIdx.x - lh * per);
-  int s, first;
-  locate_item(c.S, at, [&](int sq) { return (held_tokens(c, sq) + kGatherThreads - 1) / kGatherThreads; },
-              s, first);
-  if (s < 0) return;
-  s = uniform(s);
-  const int j = (at - first) * kGatherThreads + (int)threadIdx.x;
-  if (j >= held_const(c, s)) return;
-  const int l = uniform(lh / c.H), h = lh - l * c.H;
-  const int seq_row = read_const(c.cu_rows, s), tiles = (a.G + 15) / 16;
-  const float cl2 = a.scale * kLog2e;
-  const float2* __restrict__ norms = a.norms + ((size_t)l * c.S + s) * a.Hq + h * a.G;
-  float w = 0.f;
-  for (int t = 0; t < tiles; ++t) {
-    const float* __restrict__ z = a.logits + logits_at(a, lh * tiles + t, seq_row, s) + token_at(a, j);
-    const int heads = min(a.G - 16 * t, 16);
-#pragma unroll 4
-    for (int g = 0; g < heads; ++g) w += weight_of(z[g * kTile], cl2, norms[16 * t + g]);
-  }
-  c.weights[(size_t)lh * c.rows + seq_row + j] += w;
-}
-
 int64_t units_of(const Attend8Args& a) { return (int64_t)a.c.L * a.c.H * ((a.G + 15) / 16); }
+// The merge: one query head a workgroup while there are few.
+bool merges_heads(const Attend8Args& a) { return units_of(a) * a.c.S >= 512; }
 int64_t gather_workgroups(const Attend8Args& a) {
-  return (int64_t)a.c.L * a.c.H * (a.c.rows / kGatherThreads + a.c.S);
+  return (int64_t)a.c.L * a.c.H * (a.c.rows / (4 * (merges_heads(a) ? kMergeThreads : kMergeOne)) + a.c.S);
 }
 
 }  // namespace
@@ -500,12 +545,13 @@ void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host) {
   }
   const int64_t rows = units * a.c.S;  // workgroups of one split a sequence
   const int64_t most_single = rows > 256 ? 1024 : std::min<int64_t>(2048, 640 + 12 * rows);
-  a.single = longest * (a.c.d + 64) / 192 <= most_single;
+  a.single = longest * (a.c.d + 64) / 192 <= most_single && a.G <= 16;
   if (a.single) {
     a.splits = a.c.S;
     return;
   }
-  const int64_t want = std::max<int64_t>((1024 + units - 1) / units, total / 4096);
+  const int64_t split_rows = longest >= 32768 ? 8192 : 4096;
+  const int64_t want = std::max<int64_t>((1024 + units - 1) / units, total / split_rows);
   a.splits = (int)std::max<int64_t>(std::min<int64_t>(most, want + a.c.S), 1);
 }
 
@@ -521,8 +567,9 @@ size_t attend8_logits(const Attend8Args& a) {
 bool attend8_fits(const Attend8Args& a, bool gather) {
   // 8 waves a workgroup only where there are few; the merge's where there are many
   return grid_fits((units_of(a) * a.splits + 7) / 8 * 8, kWaves * kWave) &&
-         (a.single || grid_fits(units_of(a) * a.c.S, kMergeThreads)) &&
-         (!gather || grid_fits(gather_workgroups(a), kGatherThreads));
+         (a.single || grid_fits(units_of(a) * a.c.S * (merges_heads(a) ? 1 : std::min(a.G, 16)) +
+                                    (gather ? gather_workgroups(a) : 0),
+                                merges_heads(a) ? kMergeThreads : kMergeOne));
 }
 
 namespace {
@@ -544,18 +591,19 @@ void launch_attend(const Attend8Args& a, hipStream_t st) {
   };
   if (a.single && grid.x <= 256) run(std::integral_constant<int, 8>{});
   else run(std::integral_constant<int, kWaves>{});
-  if (!a.single) {
-    const unsigned rows = units * (unsigned)a.c.S;
-    if (rows >= 512)
-      hipLaunchKernelGGL((combine8_kernel<D, kMergeThreads, false>), dim3(rows), dim3(kMergeThreads),
-                         0, st, a);
+  if (a.single) return;
+  const unsigned rows = units * (unsigned)a.c.S, gathers = a.logits ? (unsigned)gather_workgroups(a) : 0u;
+  auto merge = [&](auto gather) {
+    constexpr bool GATHER = decltype(gather)::value;
+    if (merges_heads(a))
+      hipLaunchKernelGGL((combine8_kernel<D, kMergeThreads, false, GATHER>), dim3(gathers + rows),
+                         dim3(kMergeThreads), 0, st, a, (int)gathers);
     else
-      hipLaunchKernelGGL((combine8_kernel<D, 512, true>), dim3(rows * std::min(a.G, 16)), dim3(512),
-                         0, st, a);
-  }
-  if (a.logits && (!a.single || a.G > 16))
-    hipLaunchKernelGGL(gather8_kernel, dim3((unsigned)gather_workgroups(a)), dim3(kGatherThreads), 0,
-                       st, a);
+      hipLaunchKernelGGL((combine8_kernel<D, kMergeOne, true, GATHER>),
+                         dim3(gathers + rows * std::min(a.G, 16)), dim3(kMergeOne), 0, st, a, (int)gathers);
+  };
+  if (a.logits) merge(std::integral_constant<bool, true>{});
+  else merge(std::integral_constant<bool, false>{});
 }
 
 }  // namespace

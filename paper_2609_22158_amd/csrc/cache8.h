@@ -63,7 +63,6 @@ struct Attend8Args {
   float* lse;                // [L][S][Hq] or null
   float* partial;            // [L*H*tiles][splits][min(G, 16)][d+2]: o, m (log2), z
   float* logits;             // gather: the logits, unscaled, by tiles of tokens; or null
-  float2* norms;             // gather: [L][S][Hq] reference (log2) and 1 / sum
   int Hq, G;
   int splits;                // split slots of a (layer, KV head)
   int min_rows;              // least rows of a split

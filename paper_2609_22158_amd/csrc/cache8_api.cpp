@@ -90,19 +90,15 @@ Attend8Args attend_args(const stepkv_cache8* c, int32_t num_q_heads) {
   return a;
 }
 
-// The workspace of a decode step: the splits' states; to gather, the logits and
-// what the softmax of each row divides by.
+// The workspace of a decode step: the splits' states and, to gather, the logits.
 size_t partial_bytes(const Attend8Args& a) {
   return align_up(sizeof(float) * attend8_partial_floats(a));
 }
 size_t logits_bytes(const Attend8Args& a) {
   return align_up(sizeof(float) * attend8_logits(a));
 }
-size_t norms_bytes(const Attend8Args& a) {
-  return align_up(sizeof(float2) * (size_t)a.c.L * a.c.S * a.Hq);
-}
 size_t decode_bytes(const Attend8Args& a, bool gather) {
-  return partial_bytes(a) + (gather ? logits_bytes(a) + norms_bytes(a) : 0);
+  return partial_bytes(a) + (gather ? logits_bytes(a) : 0);
 }
 
 Evict8Args evict_args(const stepkv_cache8* c, int32_t keep, const int32_t* keeps) {
@@ -246,10 +242,7 @@ int stepkv_cache8_decode(const stepkv_cache8* c, int32_t num_q_heads, const void
   a.out = out;
   a.lse = lse;
   a.partial = reinterpret_cast<float*>(ws);
-  if (gather && a.c.rows > 0) {
-    a.logits = reinterpret_cast<float*>(ws + partial_bytes(a));
-    a.norms = reinterpret_cast<float2*>(ws + partial_bytes(a) + logits_bytes(a));
-  }
+  if (gather && a.c.rows > 0) a.logits = reinterpret_cast<float*>(ws + partial_bytes(a));
   a.scale = scale > 0.0f ? scale : (float)(1.0 / std::sqrt((double)c->head_dim));
   return hip_status(launch_attend8(a, static_cast<hipStream_t>(stream)));
 }
