@@ -63,6 +63,36 @@ __device__ __forceinline__ int rows_per_split(const Attend8Args& a) {
   return (int)((max(rows, (int64_t)a.min_rows) + a.min_rows - 1) / a.min_rows * a.min_rows);
 }
 
+// The rank-th split in order of length, of at most 64 sequences: whole splits, then
+// the sequences' last ones, the longest first. Its sequence, that one's first split,
+// and (in rank) its number in the order of the sequences; false past the last.
+__device__ __forceinline__ bool longest_first(const Attend8Args& a, int split, int& rank, int& s,
+                                              int& first) {
+  const int lane = threadIdx.x & 63;
+  const int n = lane < a.c.S ? held_tokens(a.c, lane) : 0;
+  const int whole = n / split, rest = n - whole * split;
+  const int wholes = wave_scan(whole), all = wave_total(wholes);
+  const int incl = wave_scan(whole + (rest > 0));
+  int at;  // the split's number in its sequence
+  if (rank < all) {
+    s = __builtin_ctzll(ballot(wholes > rank));
+    at = rank - __builtin_amdgcn_readlane(wholes - whole, s);
+  } else {
+    int before = 0;  // sequences whose last split is longer, or as long and of a lower index
+    for (int j = 0; j < a.c.S; ++j) {
+      const int other = __builtin_amdgcn_readlane(rest, j);
+      before += other > rest || (other == rest && j < lane);
+    }
+    const uint64_t found = ballot(rest > 0 && before == rank - all);
+    if (found == 0ull) return false;
+    s = __builtin_ctzll(found);
+    at = __builtin_amdgcn_readlane(whole, s);
+  }
+  first = __builtin_amdgcn_readlane(incl - whole - (rest > 0), s);
+  rank = first + at;
+  return true;
+}
+
 // Byte offset of piece j (16 channels) of row r in a wave's V tile, row-major:
 // with the XORs the writes (whole rows) and the transposing reads (16 bytes of
 // each of the 16 rows that two groups of 16 lanes take) touch every bank once.
@@ -125,10 +155,18 @@ void attend8_kernel(Attend8Args a) {
   const int g4 = lane >> 4, c16 = lane & 15;
   if (blockIdx.x == 0 && wave == 0) report_rooms(c);
   // Workgroups are dealt to the 8 XCDs in turn; each XCD takes a contiguous
-  // eighth of the splits.
-  const int bid = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
-  const int unit = uniform(bid / a.splits);  // (layer, KV head, 16 query heads)
-  const int gs = uniform(bid - unit * a.splits);
+  // eighth of the splits or, in batches, of the units, and their longest splits first.
+  const int xcd = (int)(blockIdx.x & 7), nth = (int)(blockIdx.x >> 3);
+  int unit, gs;  // (layer, KV head, 16 query heads); its split
+  if (a.by_length) {
+    const int units = (int)(gridDim.x >> 3) / a.splits;  // of an XCD
+    gs = uniform(nth / units);
+    unit = uniform(xcd * units + (nth - gs * units));
+  } else {
+    const int bid = xcd * (int)(gridDim.x >> 3) + nth;
+    unit = uniform(bid / a.splits);
+    gs = uniform(bid - unit * a.splits);
+  }
   const int tiles = (a.G + 15) / 16;
   if (unit >= c.L * c.H * tiles) return;  // the grid is padded to a multiple of 8
   const int lh = uniform(unit / tiles), hd0 = 16 * (unit - lh * tiles);  // first head of the group
@@ -141,9 +179,13 @@ void attend8_kernel(Attend8Args a) {
   } else {
     int first;
     const int split = rows_per_split(a);
-    locate_item(c.S, gs, [&](int sq) { return (held_tokens(c, sq) + split - 1) / split; }, s,
-                first);
-    if (s < 0) return;  // past the last split: uniform over the workgroup
+    if (a.by_length) {
+      if (!longest_first(a, split, gs, s, first)) return;
+    } else {
+      locate_item(c.S, gs, [&](int sq) { return (held_tokens(c, sq) + split - 1) / split; }, s,
+                  first);
+      if (s < 0) return;  // past the last split: uniform over the workgroup
+    }
     w0 = (gs - first) * split + wave * (split / NW);
     w1 = w0 + split / NW;
   }
@@ -521,6 +563,10 @@ __global__ __launch_bounds__(THREADS) void combine8_kernel(Attend8Args a, int ga
 }
 
 int64_t units_of(const Attend8Args& a) { return (int64_t)a.c.L * a.c.H * ((a.G + 15) / 16); }
+// Workgroups of the attention, as many for each of the 8 XCDs.
+int64_t attend_workgroups(const Attend8Args& a) {
+  return a.by_length ? (units_of(a) + 7) / 8 * 8 * a.splits : (units_of(a) * a.splits + 7) / 8 * 8;
+}
 // The merge: one query head a workgroup while there are few.
 bool merges_heads(const Attend8Args& a) { return units_of(a) * a.c.S >= 512; }
 int64_t gather_workgroups(const Attend8Args& a) {
@@ -546,6 +592,7 @@ void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host) {
   const int64_t rows = units * a.c.S;  // workgroups of one split a sequence
   const int64_t most_single = rows > 256 ? 1024 : std::min<int64_t>(2048, 640 + 12 * rows);
   a.single = longest * (a.c.d + 64) / 192 <= most_single && a.G <= 16;
+  a.by_length = 0;
   if (a.single) {
     a.splits = a.c.S;
     return;
@@ -553,6 +600,7 @@ void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host) {
   const int64_t split_rows = longest >= 32768 ? 8192 : 4096;
   const int64_t want = std::max<int64_t>((1024 + units - 1) / units, total / split_rows);
   a.splits = (int)std::max<int64_t>(std::min<int64_t>(most, want + a.c.S), 1);
+  a.by_length = a.c.S > 1 && a.c.S <= kWave && units >= 64;
 }
 
 size_t attend8_partial_floats(const Attend8Args& a) {
@@ -566,7 +614,7 @@ size_t attend8_logits(const Attend8Args& a) {
 
 bool attend8_fits(const Attend8Args& a, bool gather) {
   // 8 waves a workgroup only where there are few; the merge's where there are many
-  return grid_fits((units_of(a) * a.splits + 7) / 8 * 8, kWaves * kWave) &&
+  return grid_fits(attend_workgroups(a), kWaves * kWave) &&
          (a.single || grid_fits(units_of(a) * a.c.S * (merges_heads(a) ? 1 : std::min(a.G, 16)) +
                                     (gather ? gather_workgroups(a) : 0),
                                 merges_heads(a) ? kMergeThreads : kMergeOne));
@@ -577,7 +625,7 @@ namespace {
 template <int D>
 void launch_attend(const Attend8Args& a, hipStream_t st) {
   const unsigned units = (unsigned)units_of(a);
-  const dim3 grid((units * (unsigned)a.splits + 7u) / 8u * 8u);
+  const dim3 grid((unsigned)attend_workgroups(a));
   auto copies = [&](auto nw, auto cc) {
     constexpr int NW = decltype(nw)::value, C = decltype(cc)::value;
     if (a.logits)

@@ -67,9 +67,10 @@ struct Attend8Args {
   int splits;                // split slots of a (layer, KV head)
   int min_rows;              // least rows of a split
   int single;                // nonzero: a sequence is one split, written without a merge
+  int by_length;             // nonzero: the longest splits are taken first
   float scale;
 };
-// Fills splits, min_rows and single from the shape and the rooms of the sequences.
+// Fills splits, min_rows, single and by_length from the shape and the rooms of the sequences.
 void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host);
 size_t attend8_partial_floats(const Attend8Args& a);
 size_t attend8_logits(const Attend8Args& a);  // floats of them
