@@ -74,12 +74,17 @@ _NONE_BELOW = ("stepkv_cache4_decode_workspace_bytes", "stepkv_cache8_decode_wor
 
 _lib: Optional[ctypes.CDLL] = None
 _fns: dict = {}  # the library's functions by name
+torch = None  # imported with the library, not with this module (nor in every call: 0.2 us each)
+_raw_stream = None  # torch's call for the raw handle of a device's current stream, where it has one
 
 
 def load() -> ctypes.CDLL:
     """The library with the signatures of stepkv_cache4.h declared."""
-    global _lib
+    global _lib, torch, _raw_stream
     if _lib is None:
+        import torch as module
+
+        torch, _raw_stream = module, getattr(module._C, "_cuda_getCurrentRawStream", None)
         lib = B.load()
         declare(lib, _SIGNATURES)
         _fns["stepkv_status_read"] = lib.stepkv_status_read
@@ -208,15 +213,14 @@ def _need(t, dtype, shape, name, device):
 
 def _call(cache, name, stream, *args):
     """The library's `name` on the cache's device; the stream is the last argument."""
-    import torch
-
     dev = cache.device
     if dev.type != "cuda":
         raise ValueError(f"{name}: the cache lies on {dev}, not on a GPU")
     if stream is not None and stream.device != dev:
         raise ValueError(f"{name}: a stream of {stream.device}, the cache lies on {dev}")
     if torch.cuda.current_device() == dev.index:
-        rc = _fns[name](*args, B._stream(stream))
+        handle = B._stream(stream) if stream is not None or _raw_stream is None else _raw_stream(dev.index)
+        rc = _fns[name](*args, handle)
     else:
         with torch.cuda.device(dev):
             rc = _fns[name](*args, B._stream(stream))
@@ -226,8 +230,6 @@ def _call(cache, name, stream, *args):
 
 def _empty(shape, dtype, cache, stream):
     """A buffer for a call: of the stream that the call runs on."""
-    import torch
-
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=cache.device)
     with torch.cuda.stream(stream):
@@ -237,8 +239,6 @@ def _empty(shape, dtype, cache, stream):
 def _workspace(workspace, cache, stream, size, *args):
     """The caller's workspace, or one of `size`(cache, *args) bytes: that depends on the shape alone,
     which a cache keeps."""
-    import torch
-
     if workspace is None:
         key = (size, args)
         nbytes = cache._sizes.get(key)
@@ -261,8 +261,6 @@ def compact4(pb: B.Problem, cache: Cache4, k, v, idx, cu_retained, *, stream=Non
     """stepkv_cache4_compact: the retained rows into the cache, quantised; sets cache.lens.
 
     idx is [L][Hkv][Ntot] (compact's) or [Ntot] (compact_shared's)."""
-    import torch
-
     L, H, d, dev = pb.num_layers, pb.num_kv_heads, pb.head_dim, cache.device
     if pb.cu_seqlens_dev.device != dev:
         raise ValueError(f"pb: lies on {pb.cu_seqlens_dev.device}, the cache on {dev}")
@@ -278,8 +276,6 @@ def compact4(pb: B.Problem, cache: Cache4, k, v, idx, cu_retained, *, stream=Non
 
 def advance4(cache: Cache4, cu_new, *, stream=None) -> Cache4:
     """stepkv_cache4_advance: lens[s] += cu_new[s + 1] - cu_new[s], once for all layers."""
-    import torch
-
     cp = _need(cu_new, torch.int32, (cache.num_seqs + 1,), "cu_new", cache.device)
     _call(cache, "stepkv_cache4_advance", stream, cache._ref, cp)
     return cache
@@ -287,8 +283,6 @@ def advance4(cache: Cache4, cu_new, *, stream=None) -> Cache4:
 
 def _tokens(t, cache, name):
     """Pointer and strides of new tokens bf16 [L][T][Hkv][d] whose channels are contiguous."""
-    import torch
-
     if t.dtype != torch.bfloat16:
         raise TypeError(f"{name}: dtype {t.dtype}, expected {torch.bfloat16}")
     key = (t.shape, t.stride())
@@ -314,8 +308,6 @@ def append4(cache: Cache4, k_new, v_new, cu_new, *, stream=None) -> Cache4:
     """stepkv_cache4_append: new tokens bf16 [L][T][Hkv][d] (any strides over layers, tokens and
     heads; tokens cu_new[s] .. cu_new[s + 1] - 1 are sequence s's) as its last tokens. Call
     advance4 before, once for all layers."""
-    import torch
-
     kp, ks = _tokens(k_new, cache, "k_new")
     vp, vs = _tokens(v_new, cache, "v_new")
     if v_new.shape != k_new.shape:
@@ -334,8 +326,6 @@ def read4(cache: Cache4, cu_out, out_rows: int, *, k_out=None, v_out=None, strea
 
 
 def _read(cache, name, cu_out, out_rows, k_out, v_out, stream):
-    import torch
-
     shape = (cache.num_layers, cache.num_kv_heads, int(out_rows), cache.head_dim)
     cp = _need(cu_out, torch.int32, (cache.num_seqs + 1,), "cu_out", cache.device)
 
@@ -354,8 +344,6 @@ def _read(cache, name, cu_out, out_rows, k_out, v_out, stream):
 
 # ---------------------------------------------------------------- attention
 def _queries(cache, q_dec):
-    import torch
-
     if q_dec.dim() != 4:
         raise ValueError(f"q_dec: shape {tuple(q_dec.shape)}, expected [L][S][Hq][d]")
     Hq = int(q_dec.shape[2])
@@ -364,8 +352,6 @@ def _queries(cache, q_dec):
 
 
 def _results(cache, Hq, out, lse, want_lse, stream):
-    import torch
-
     L, S, d = cache.num_layers, cache.num_seqs, cache.head_dim
     if out is None:
         out = _empty((L, S, Hq, d), torch.float32, cache, stream)
@@ -383,8 +369,6 @@ def decode_attention4(cache: Cache4, q_dec, *, blocks=None, scale: float = 0.0, 
     """stepkv_cache4_decode: fp32 [L][S][Hq][d], over all tokens or the listed blocks (int32
     [L][S][Hkv][n], n >= 1, as select_blocks4 gives them). With ``want_lse`` or an ``lse`` buffer also
     the rows' natural-log log-sum-exps [L][S][Hq]: (out, lse)."""
-    import torch
-
     qp, Hq = _queries(cache, q_dec)
     bp, n = None, 0
     if blocks is not None:
@@ -401,8 +385,6 @@ def decode_attention4(cache: Cache4, q_dec, *, blocks=None, scale: float = 0.0, 
 
 
 def _blocks(cache, num_blocks, blocks, stream):
-    import torch
-
     shape = (cache.num_layers, cache.num_seqs, cache.num_kv_heads, int(num_blocks))
     if num_blocks < 1:
         raise ValueError("num_blocks: one block at least")

@@ -69,14 +69,16 @@ _SIGNATURES = {
 }
 
 _loaded = False
+torch = None  # imported with the library
 
 
 def load() -> ctypes.CDLL:
     """The library with the signatures of stepkv_cache8.h declared."""
-    global _loaded
+    global _loaded, torch
     lib = C4.load()
     if not _loaded:
         C4.declare(lib, _SIGNATURES)
+        torch = C4.torch
         _loaded = True
     return lib
 
@@ -174,8 +176,6 @@ def compact8(pb: B.Problem, cache: Cache8, k, v, idx, cu_retained, *, weights=No
 
     idx is [L][Hkv][Ntot] (compact's) or [Ntot] (compact_shared's). weights (fp32 [L][Hkv][Ntot],
     e.g. the saliency) is what the source's tokens gathered so far; without it they start at 0."""
-    import torch
-
     L, H, d, dev = pb.num_layers, pb.num_kv_heads, pb.head_dim, cache.device
     if pb.cu_seqlens_dev.device != dev:
         raise ValueError(f"pb: lies on {pb.cu_seqlens_dev.device}, the cache on {dev}")
@@ -197,8 +197,6 @@ def compact8(pb: B.Problem, cache: Cache8, k, v, idx, cu_retained, *, weights=No
 def advance8(cache: Cache8, cu_new, *, stream=None) -> Cache8:
     """stepkv_cache8_advance: lens[s] and seen[s] += cu_new[s + 1] - cu_new[s], once for all
     layers."""
-    import torch
-
     cp = C4._need(cu_new, torch.int32, (cache.num_seqs + 1,), "cu_new", cache.device)
     C4._call(cache, "stepkv_cache8_advance", stream, cache._ref, cp)
     return cache
@@ -208,8 +206,6 @@ def append8(cache: Cache8, k_new, v_new, cu_new, *, stream=None) -> Cache8:
     """stepkv_cache8_append: new tokens bf16 [L][T][Hkv][d] (any strides over layers, tokens and
     heads; tokens cu_new[s] .. cu_new[s + 1] - 1 are sequence s's) as its last tokens. Call
     advance8 before, once for all layers."""
-    import torch
-
     kp, ks = C4._tokens(k_new, cache, "k_new")
     vp, vs = C4._tokens(v_new, cache, "v_new")
     if v_new.shape != k_new.shape:
@@ -251,8 +247,6 @@ def evict8(cache: Cache8, keep: int = 0, *, keeps=None, first: int = 0, recent: 
     ``keeps``, int32 [S] on the device): those of least gathered weight, apart from positions below
     ``first`` and the last ``recent`` ones. Each head its own, so this takes the whole cache, not
     some of its layers; cache.positions says which tokens stay, and cache.lens how many."""
-    import torch
-
     if not cache.whole:
         raise ValueError("evict8: takes all layers of a cache, whose lens they share")
     if cache.weights is None:
