@@ -150,7 +150,7 @@ int stepkv_cache8_read(const stepkv_cache8* c, const int32_t* cu_out, int32_t ou
 
 /* Bytes of device workspace stepkv_cache8_decode needs for num_q_heads query
  * heads (0 when invalid). 256: the call needs none, and takes NULL (short
- * sequences, which are not split, and no gathering). */
+ * sequences, which are not split, without gathering or a few of them). */
 size_t stepkv_cache8_decode_workspace_bytes(const stepkv_cache8* c, int32_t num_q_heads,
                                             int32_t gather);
 

@@ -39,6 +39,8 @@ typedef __attribute__((address_space(3))) i32x2_t lds_i32x2;
 
 constexpr int kTile = 32;  // tokens a wave computes at a time
 constexpr int kWaves = 4;  // waves of a workgroup
+constexpr int kWavesFew = 8;  // where a whole sequence is one, and there are few
+constexpr int kMostLds = 32768;  // bytes of logits kept in LDS
 constexpr int kMergeThreads = 256;  // of a merge of many rows
 constexpr int kMergeOne = 512;      // and of a merge of one query head
 constexpr float kSlack = 16.f;
@@ -132,9 +134,12 @@ __device__ __forceinline__ float weight_of(float y, float cl2, float2 norm) {
   return fast_exp2(fmaf(y, cl2, -norm.x)) * norm.y;
 }
 
+// Where the logits that weights are gathered from are kept.
+enum { kNone, kMemory, kLds };
+
 // NW waves share a split (or, with a.single, a whole sequence); C copies (1 or 3)
 // of the query heads in the operands' rows.
-template <int D, int NW, bool GATHER, int C>
+template <int D, int NW, int GATHER, int C>
 __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(3)))
 void attend8_kernel(Attend8Args a) {
   constexpr int KP = D / 64;        // 16-byte K pieces of a row that a lane loads
@@ -215,7 +220,10 @@ void attend8_kernel(Attend8Args a) {
   uint8_t* const vt = smem + wave * TB;
   const int vrow = lane / VP, vpiece = lane % VP;  // this lane's V row and piece
   // the logits of this lane's head and rows, from the sequence's first tile
-  float* const zt = GATHER ? a.logits + logits_at(a, unit, seq_row, s) + c16 * kTile + 4 * g4 : nullptr;
+  extern __shared__ __attribute__((aligned(16))) float zlds[];
+  float* const zt =
+      (GATHER == kLds ? zlds : GATHER == kMemory ? a.logits + logits_at(a, unit, seq_row, s) : nullptr) +
+      c16 * kTile + 4 * g4;
 
   struct Tile {
     u32x4_t k[2][KP], v[VL];
@@ -323,7 +331,7 @@ void attend8_kernel(Attend8Args a) {
       const float vs = cur.vs;
       consume(cur);
       // before the loads, whose wait then is for nothing else
-      if (GATHER && c16 < heads) {  // the first copy's lanes; a tile has room for all its rows
+      if (GATHER != kNone && c16 < heads) {  // the first copy's lanes; a tile has room for all its rows
         f32x4_t* const z4 = reinterpret_cast<f32x4_t*>(zt + (size_t)t * min(a.G, 16) * kTile);
         z4[0] = acc[0];
         z4[4] = acc[1];
@@ -368,7 +376,7 @@ void attend8_kernel(Attend8Args a) {
     }
     if (a.single) {
       finish(a, row_out + hd, ch, D, M, Z, O);
-      if (GATHER && ch == 0) norm_s[hd] = make_float2(M, 1.f / Z);
+      if (GATHER != kNone && ch == 0) norm_s[hd] = make_float2(M, 1.f / Z);
       continue;
     }
     part[hd * ST + ch] = O;
@@ -377,12 +385,12 @@ void attend8_kernel(Attend8Args a) {
       part[hd * ST + D + 1] = Z;
     }
   }
-  if constexpr (GATHER) {
+  if constexpr (GATHER != kNone) {
     // All heads' logits of the whole sequence are this workgroup's: their weights.
     if (!a.single) return;
     __threadfence_block();
     __syncthreads();
-    const float* __restrict__ base = a.logits + logits_at(a, unit, seq_row, s);
+    const float* const base = zt - (c16 * kTile + 4 * g4);
     for (int j = tid; j < held; j += NW * kWave) {
       float w = 0.f;
       for (int g = 0; g < heads; ++g)
@@ -567,6 +575,7 @@ int64_t units_of(const Attend8Args& a) { return (int64_t)a.c.L * a.c.H * ((a.G +
 int64_t attend_workgroups(const Attend8Args& a) {
   return a.by_length ? (units_of(a) + 7) / 8 * 8 * a.splits : (units_of(a) * a.splits + 7) / 8 * 8;
 }
+bool few_workgroups(const Attend8Args& a) { return a.single && attend_workgroups(a) <= 256; }
 // The merge: one query head a workgroup while there are few.
 bool merges_heads(const Attend8Args& a) { return units_of(a) * a.c.S >= 512; }
 int64_t gather_workgroups(const Attend8Args& a) {
@@ -592,9 +601,12 @@ void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host) {
   const int64_t rows = units * a.c.S;  // workgroups of one split a sequence
   const int64_t most_single = rows > 256 ? 1024 : std::min<int64_t>(2048, 640 + 12 * rows);
   a.single = longest * (a.c.d + 64) / 192 <= most_single && a.G <= 16;
-  a.by_length = 0;
+  a.by_length = a.lds_bytes = 0;
   if (a.single) {
     a.splits = a.c.S;
+    // few workgroups: a CU's LDS has room for the logits of a short sequence
+    const int64_t bytes = (longest + kTile - 1) / kTile * a.G * kTile * (int64_t)sizeof(float);
+    if (few_workgroups(a) && bytes <= kMostLds) a.lds_bytes = (int)bytes;
     return;
   }
   const int64_t split_rows = longest >= 32768 ? 8192 : 4096;
@@ -609,14 +621,15 @@ size_t attend8_partial_floats(const Attend8Args& a) {
 }
 
 size_t attend8_logits(const Attend8Args& a) {
+  if (a.lds_bytes > 0) return 0;
   return (size_t)units_of(a) * (a.c.rows / kTile + a.c.S) * std::min(a.G, 16) * kTile;
 }
 
-bool attend8_fits(const Attend8Args& a, bool gather) {
+bool attend8_fits(const Attend8Args& a) {
   // 8 waves a workgroup only where there are few; the merge's where there are many
   return grid_fits(attend_workgroups(a), kWaves * kWave) &&
          (a.single || grid_fits(units_of(a) * a.c.S * (merges_heads(a) ? 1 : std::min(a.G, 16)) +
-                                    (gather ? gather_workgroups(a) : 0),
+                                    (a.gather ? gather_workgroups(a) : 0),
                                 merges_heads(a) ? kMergeThreads : kMergeOne));
 }
 
@@ -628,19 +641,21 @@ void launch_attend(const Attend8Args& a, hipStream_t st) {
   const dim3 grid((unsigned)attend_workgroups(a));
   auto copies = [&](auto nw, auto cc) {
     constexpr int NW = decltype(nw)::value, C = decltype(cc)::value;
-    if (a.logits)
-      hipLaunchKernelGGL((attend8_kernel<D, NW, true, C>), grid, dim3(NW * kWave), 0, st, a);
-    else
-      hipLaunchKernelGGL((attend8_kernel<D, NW, false, C>), grid, dim3(NW * kWave), 0, st, a);
+    if (!a.gather)
+      hipLaunchKernelGGL((attend8_kernel<D, NW, kNone, C>), grid, dim3(NW * kWave), 0, st, a);
+    else if (a.lds_bytes == 0)
+      hipLaunchKernelGGL((attend8_kernel<D, NW, kMemory, C>), grid, dim3(NW * kWave), 0, st, a);
+    else if constexpr (NW == kWavesFew)
+      hipLaunchKernelGGL((attend8_kernel<D, NW, kLds, C>), grid, dim3(NW * kWave), a.lds_bytes, st, a);
   };
   auto run = [&](auto nw) {
     if (a.G <= 5) copies(nw, std::integral_constant<int, 3>{});
     else copies(nw, std::integral_constant<int, 1>{});
   };
-  if (a.single && grid.x <= 256) run(std::integral_constant<int, 8>{});
+  if (few_workgroups(a)) run(std::integral_constant<int, kWavesFew>{});
   else run(std::integral_constant<int, kWaves>{});
   if (a.single) return;
-  const unsigned rows = units * (unsigned)a.c.S, gathers = a.logits ? (unsigned)gather_workgroups(a) : 0u;
+  const unsigned rows = units * (unsigned)a.c.S, gathers = a.gather ? (unsigned)gather_workgroups(a) : 0u;
   auto merge = [&](auto gather) {
     constexpr bool GATHER = decltype(gather)::value;
     if (merges_heads(a))
@@ -650,7 +665,7 @@ void launch_attend(const Attend8Args& a, hipStream_t st) {
       hipLaunchKernelGGL((combine8_kernel<D, kMergeOne, true, GATHER>),
                          dim3(gathers + rows * std::min(a.G, 16)), dim3(kMergeOne), 0, st, a, (int)gathers);
   };
-  if (a.logits) merge(std::integral_constant<bool, true>{});
+  if (a.gather) merge(std::integral_constant<bool, true>{});
   else merge(std::integral_constant<bool, false>{});
 }
 

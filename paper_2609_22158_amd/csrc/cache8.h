@@ -62,19 +62,21 @@ struct Attend8Args {
   float* out;                // [L][S][Hq][d]
   float* lse;                // [L][S][Hq] or null
   float* partial;            // [L*H*tiles][splits][min(G, 16)][d+2]: o, m (log2), z
-  float* logits;             // gather: the logits, unscaled, by tiles of tokens; or null
+  float* logits;             // gather: the logits, unscaled, by tiles of tokens
   int Hq, G;
   int splits;                // split slots of a (layer, KV head)
   int min_rows;              // least rows of a split
   int single;                // nonzero: a sequence is one split, written without a merge
   int by_length;             // nonzero: the longest splits are taken first
+  int gather;                // nonzero: weights are added up
+  int lds_bytes;             // of the logits, where LDS holds them (then logits is null)
   float scale;
 };
-// Fills splits, min_rows, single and by_length from the shape and the rooms of the sequences.
+// Fills splits, min_rows, single, by_length and lds_bytes from the shape and the rooms of the sequences.
 void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host);
 size_t attend8_partial_floats(const Attend8Args& a);
 size_t attend8_logits(const Attend8Args& a);  // floats of them
-bool attend8_fits(const Attend8Args& a, bool gather);
+bool attend8_fits(const Attend8Args& a);
 hipError_t launch_attend8(const Attend8Args& a, hipStream_t st);
 
 // ---------------------------------------------------------------- eviction

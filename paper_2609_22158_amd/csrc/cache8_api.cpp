@@ -81,9 +81,10 @@ Cache8View view(const stepkv_cache8* c) {
   return w;
 }
 
-Attend8Args attend_args(const stepkv_cache8* c, int32_t num_q_heads) {
+Attend8Args attend_args(const stepkv_cache8* c, int32_t num_q_heads, int32_t gather) {
   Attend8Args a{};
   a.c = view(c);
+  a.gather = gather != 0 && a.c.rows > 0;
   a.Hq = num_q_heads;
   a.G = num_q_heads / c->num_kv_heads;
   plan_attend8(a, c->cu_rows_host);
@@ -97,8 +98,8 @@ size_t partial_bytes(const Attend8Args& a) {
 size_t logits_bytes(const Attend8Args& a) {
   return align_up(sizeof(float) * attend8_logits(a));
 }
-size_t decode_bytes(const Attend8Args& a, bool gather) {
-  return partial_bytes(a) + (gather ? logits_bytes(a) : 0);
+size_t decode_bytes(const Attend8Args& a) {
+  return partial_bytes(a) + (a.gather ? logits_bytes(a) : 0);
 }
 
 Evict8Args evict_args(const stepkv_cache8* c, int32_t keep, const int32_t* keeps) {
@@ -219,7 +220,7 @@ int stepkv_cache8_read(const stepkv_cache8* c, const int32_t* cu_out, int32_t ou
 size_t stepkv_cache8_decode_workspace_bytes(const stepkv_cache8* c, int32_t num_q_heads,
                                             int32_t gather) {
   if (check_cache(c) != STEPKV_OK || check_heads(c, num_q_heads) != STEPKV_OK) return 0;
-  return std::max(decode_bytes(attend_args(c, num_q_heads), gather != 0), kAlign);
+  return std::max(decode_bytes(attend_args(c, num_q_heads, gather)), kAlign);
 }
 
 int stepkv_cache8_decode(const stepkv_cache8* c, int32_t num_q_heads, const void* q_dec,
@@ -232,9 +233,9 @@ int stepkv_cache8_decode(const stepkv_cache8* c, int32_t num_q_heads, const void
   // the kernel scales logits by scale * log2(e): 0 times an infinity is NaN
   if (scale > 0.0f && !std::isfinite(scale * 1.44269504088896341f)) return STEPKV_EINVAL;
   if (gather && !gathers(c)) return STEPKV_EINVAL;
-  Attend8Args a = attend_args(c, num_q_heads);
-  if (!attend8_fits(a, gather != 0)) return STEPKV_EUNSUPPORTED;
-  const size_t need = decode_bytes(a, gather != 0);
+  Attend8Args a = attend_args(c, num_q_heads, gather);
+  if (!attend8_fits(a)) return STEPKV_EUNSUPPORTED;
+  const size_t need = decode_bytes(a);
   if (need > 0 && (!workspace || !aligned(workspace, kAlign) || ws_bytes < need))
     return STEPKV_EWORKSPACE;
   uint8_t* const ws = static_cast<uint8_t*>(workspace);
@@ -242,7 +243,7 @@ int stepkv_cache8_decode(const stepkv_cache8* c, int32_t num_q_heads, const void
   a.out = out;
   a.lse = lse;
   a.partial = reinterpret_cast<float*>(ws);
-  if (gather && a.c.rows > 0) a.logits = reinterpret_cast<float*>(ws + partial_bytes(a));
+  if (a.gather) a.logits = reinterpret_cast<float*>(ws + partial_bytes(a));
   a.scale = scale > 0.0f ? scale : (float)(1.0 / std::sqrt((double)c->head_dim));
   return hip_status(launch_attend8(a, static_cast<hipStream_t>(stream)));
 }
