@@ -249,6 +249,9 @@ def evict8(cache: Cache8, keep: int = 0, *, keeps=None, first: int = 0, recent: 
     some of its layers; cache.positions says which tokens stay, and cache.lens how many."""
     if not cache.whole:
         raise ValueError("evict8: takes all layers of a cache, whose lens they share")
+    for name, x in (("keep", keep), ("first", first), ("recent", recent)):
+        if not 0 <= x < 1 << 31:  # what the library takes; of more the lower bits would count
+            raise ValueError(f"{name}: {x} is not a number of tokens")
     if cache.weights is None:
         raise ValueError("evict8: the cache keeps no weights")
     if keeps is None and keep < 1:

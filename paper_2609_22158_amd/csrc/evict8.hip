@@ -7,14 +7,18 @@
 //
 // evict8_kernel: one workgroup per (layer, KV head, sequence) finds the key of the
 // keep-th best token by radix search over the weights' bits, and lists the moves.
-// A wave holds a run of consecutive rows, 64 at a time, one key a lane and
-// register; so which of them stay is a mask in scalar registers, and what waves
+// A wave holds a run of consecutive rows in registers, four a lane, and what waves
 // have to tell each other is a few totals. The weights and positions, 8 bytes a
-// token, are read once (rows past 1024 x 80: once a phase).
+// token, are read once (of rooms past 81920 rows once a phase). Loading takes half
+// its time, then LDS atomics and the chain of phases on the CU that holds a row: 28
+// layers x 4 heads x 16 sequences of 700 to 8192 rows 30 us (64 MB; 14 of them
+// loading), 64 rows of 67584 38 us (12; a quarter of the chip).
 // move8_kernel: the rows, their weights and positions, 16 moves a wave; a wave has
 // all the moves into a block, so that it can round the block's other tokens if
 // its scale grows. A block partly below `keep` is one that rows leave and others
-// enter: its scales as they were are kept by the selection.
+// enter: its scales as they were are kept by the selection. Rows of 128 bytes from
+// all over the cache and their chain of three loads bound it: 64 x 2048 moves 25 us
+// (69 MB), one in each of 1792 heads 10.
 #include "cache8_device.h"
 
 #include <algorithm>
@@ -164,88 +168,126 @@ void evict8_kernel(Evict8Args a) {
     for (int g = 0; g < NG; ++g)
       if (g < ng) load(j0 + g * kGroup + 4 * lane, keys + 4 * g);
   }
+  // Tokens that stay in any case, and the least and greatest key of the others.
+  uint32_t least1 = 0xFFFFFFFFu, most1 = 0u;  // least - 1, and most + 1
+  int always = 0;
+  each([&](int, const uint32_t* k) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {  // 0 - 1 and kStays + 1 wrap out of the way
+      least1 = min(least1, k[e] - 1u);
+      most1 = max(most1, k[e] + 1u);
+      always += k[e] == kStays;
+    }
+  });
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    least1 = min(least1, (uint32_t)__shfl_xor((int)least1, off, kWave));
+    most1 = max(most1, (uint32_t)__shfl_xor((int)most1, off, kWave));
+  }
+  always = wave_total(wave_scan(always));
+  if (lane == 0) {
+    sh.count[0][wave] = (int)least1;
+    sh.count[1][wave] = (int)most1;
+    sh.count[2][wave] = always;
+  }
   for (int i = tid; i < kBins; i += W * kWave) sh.hist[i] = 0u;
   __syncthreads();
-  // The key of the keep-th greatest, and how many of those equal to it stay: by 11
-  // bits at a time, among the keys that have tau's bits above them.
-  uint32_t tau = 0u, above = 0u, rank = (uint32_t)keep, ties;
-  for (int down = 32 - kDigit;;) {
-    each([&](int, const uint32_t* k) __attribute__((always_inline)) {
-      uint32_t bin[4];
-      bool in[4];
+  always = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        in[e] = ((k[e] ^ tau) & above) == 0u;
-        bin[e] = (k[e] >> down) & (kBins - 1);
-      }
-      const uint64_t act = ballot(in[0]);
-      // Many lanes of one bin (equal weights, tokens that stay in any case, none
-      // at all) are added as one: atomics on one word run one after another.
-      bool clustered = false;
-      if (act != 0ull) {
-        const uint32_t lead = (uint32_t)__builtin_amdgcn_readlane((int)bin[0], __builtin_ctzll(act));
-        clustered = __popcll(ballot(in[0] && bin[0] == lead)) >= 16;
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        bool add = in[e];
-        if (clustered) {  // uniform
-          const uint64_t on = ballot(add);
-          if (on == 0ull) continue;
-          const int lead = __builtin_ctzll(on);
-          const uint64_t same = ballot(add && bin[e] == (uint32_t)__builtin_amdgcn_readlane((int)bin[e], lead));
-          if (lane == lead) atomicAdd(&sh.hist[bin[e]], (uint32_t)__popcll(same));
-          add = add && !(same >> lane & 1ull);
-        }
-        if (add) atomicAdd(&sh.hist[bin[e]], 1u);
-      }
-    });
-    __syncthreads();
-    find_bin<W>(sh, rank);
-    tau |= (uint32_t)uniform((int)sh.found[0]) << down;
-    rank = (uint32_t)uniform((int)sh.found[1]);
-    ties = (uint32_t)uniform((int)sh.found[2]);
-    above = ~((1u << down) - 1u);
-    if (down == 0 || rank == ties) break;  // one key, or every key of the bin stays
-    if (ties <= kList) {  // its keys, in any order, compared with each other
+  for (int v = 0; v < W; ++v) {
+    least1 = min(least1, (uint32_t)sh.count[0][v]);
+    most1 = max(most1, (uint32_t)sh.count[1][v]);
+    always += sh.count[2][v];
+  }
+  // The key tau of the keep-th greatest, and how many of those equal to it stay: keys
+  // lo .. lo + span in 2048 bins, then those of the bin that holds it.
+  uint32_t tau, rank, ties;
+  if (always >= keep) {
+    tau = kStays;
+    rank = (uint32_t)keep;
+    ties = (uint32_t)always;
+  } else {
+    uint32_t lo = least1 + 1u, span = most1 - 1u - lo;
+    tau = lo;
+    rank = (uint32_t)(keep - always);
+    ties = (uint32_t)(n - always);
+    while (span > 0u) {
+      const int shift = max(32 - kDigit - __builtin_clz(span), 0);
       each([&](int, const uint32_t* k) __attribute__((always_inline)) {
         uint32_t d[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) d[e] = (k[e] ^ tau) & above;
-        if (min(min(d[0], d[1]), min(d[2], d[3])) == 0u) {  // few lanes hold one
+        for (int e = 0; e < 4; ++e) d[e] = k[e] - lo;
+        // Many lanes of one bin (equal weights) are added as one: atomics on one
+        // word run one after another.
+        const uint64_t act = ballot(d[0] <= span);
+        bool clustered = false;
+        if (act != 0ull) {
+          const uint32_t lead = (uint32_t)__builtin_amdgcn_readlane((int)d[0], __builtin_ctzll(act));
+          clustered = __popcll(ballot(d[0] >> shift == lead >> shift)) >= 16;
+        }
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (d[e] == 0u) sh.list[atomicAdd(&sh.listed, 1u)] = k[e];
+        for (int e = 0; e < 4; ++e) {
+          bool add = d[e] <= span;
+          const uint32_t bin = d[e] >> shift;
+          if (clustered) {  // uniform
+            const uint64_t on = ballot(add);
+            if (on == 0ull) continue;
+            const int lead = __builtin_ctzll(on);
+            const uint64_t same = ballot(add && bin == (uint32_t)__builtin_amdgcn_readlane((int)bin, lead));
+            if (lane == lead) atomicAdd(&sh.hist[bin], (uint32_t)__popcll(same));
+            add = add && !(same >> lane & 1ull);
+          }
+          if (add) atomicAdd(&sh.hist[bin], 1u);
         }
       });
       __syncthreads();
-      const int m = (int)ties;
-      if (tid < m) {
-        const uint32_t mine = sh.list[tid];
-        uint32_t gt = 0u, ge = 0u;
-        for (int i = 0; i < m; ++i) {
-          const uint32_t o = sh.list[i];
-          gt += o > mine;
-          ge += o >= mine;
-        }
-        if (gt < rank && rank <= ge) {  // equal keys write the same
-          sh.found[0] = mine;
-          sh.found[1] = rank - gt;
-          sh.found[2] = ge - gt;
-        }
-      }
-      __syncthreads();
-      tau = (uint32_t)uniform((int)sh.found[0]);
+      find_bin<W>(sh, rank);
+      lo += (uint32_t)uniform((int)sh.found[0]) << shift;
+      span = (1u << shift) - 1u;
+      tau = lo;
       rank = (uint32_t)uniform((int)sh.found[1]);
       ties = (uint32_t)uniform((int)sh.found[2]);
-      break;
+      if (rank == ties) break;  // every key of the bin stays
+      if (span > 0u && ties <= kList) {  // its keys, in any order, compared with each other
+        each([&](int, const uint32_t* k) __attribute__((always_inline)) {
+          uint32_t d[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) d[e] = k[e] - lo;
+          if (min(min(d[0], d[1]), min(d[2], d[3])) <= span) {  // few lanes hold one
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (d[e] <= span) sh.list[atomicAdd(&sh.listed, 1u)] = k[e];
+          }
+        });
+        __syncthreads();
+        const int m = (int)ties;
+        if (tid < m) {
+          const uint32_t mine = sh.list[tid];
+          uint32_t gt = 0u, ge = 0u;
+          for (int i = 0; i < m; ++i) {
+            const uint32_t o = sh.list[i];
+            gt += o > mine;
+            ge += o >= mine;
+          }
+          if (gt < rank && rank <= ge) {  // equal keys write the same
+            sh.found[0] = mine;
+            sh.found[1] = rank - gt;
+            sh.found[2] = ge - gt;
+          }
+        }
+        __syncthreads();
+        tau = (uint32_t)uniform((int)sh.found[0]);
+        rank = (uint32_t)uniform((int)sh.found[1]);
+        ties = (uint32_t)uniform((int)sh.found[2]);
+        break;
+      }
     }
-    down = max(down - kDigit, 0);
   }
   // keys above t_sure stay; of those equal to tau the first `need`, or (need 0) all
   const uint32_t t_sure = rank == ties ? tau - 1u : tau;
   const uint32_t need = rank == ties ? 0u : rank;
   uint32_t tie0 = 0u;  // ties in the rows before this wave's
+  __syncthreads();     // sh.count is read
   if (need > 0u) {
     int here = 0;
     each([&](int, const uint32_t* k) __attribute__((always_inline)) {
@@ -592,13 +634,14 @@ hipError_t launch_evict8(const Evict8Args& a, hipStream_t st) {
   };
   using std::integral_constant;
   const integral_constant<bool, false> once{};
-  const integral_constant<int, 4> four{};
-  const integral_constant<int, 16> sixteen{};
-  if (a.longest <= 4 * 256 * 2) run(four, integral_constant<int, 2>{}, once);
-  else if (a.longest <= 4 * 256 * 10) run(four, integral_constant<int, 10>{}, once);
-  else if (a.longest <= 16 * 256 * 8) run(sixteen, integral_constant<int, 8>{}, once);
-  else if (a.longest <= 16 * 256 * 20) run(sixteen, integral_constant<int, 20>{}, once);
-  else run(sixteen, integral_constant<int, 4>{}, integral_constant<bool, true>{});
+  // Waves and groups of 256 rows for the longest room: few keys a lane leave room for
+  // more workgroups (28 layers x 4 heads x 16 sequences of 700 to 8192 rows: 4 waves
+  // of 10 groups 32 us, 8 of 5 30).
+  if (a.longest <= 4 * 256 * 2) run(integral_constant<int, 4>{}, integral_constant<int, 2>{}, once);
+  else if (a.longest <= 8 * 256 * 5) run(integral_constant<int, 8>{}, integral_constant<int, 5>{}, once);
+  else if (a.longest <= 16 * 256 * 8) run(integral_constant<int, 16>{}, integral_constant<int, 8>{}, once);
+  else if (a.longest <= 16 * 256 * 20) run(integral_constant<int, 16>{}, integral_constant<int, 20>{}, once);
+  else run(integral_constant<int, 16>{}, integral_constant<int, 4>{}, integral_constant<bool, true>{});
   const dim3 grid((unsigned)move_workgroups(a));
   if (a.c.d == 128)
     hipLaunchKernelGGL(move8_kernel<128>, grid, dim3(kMoveThreads), 0, st, a);

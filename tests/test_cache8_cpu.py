@@ -285,6 +285,9 @@ def test_python_refuses_before_the_library():
         C8.evict8(c, keeps=cu)
     with pytest.raises(ValueError, match="keep"):
         C8.evict8(c)
+    for kw in (dict(keep=2 ** 32 + 5), dict(keep=-1), dict(keep=5, first=2 ** 31), dict(keep=5, recent=-2 ** 32 + 9)):
+        with pytest.raises(ValueError, match="number of tokens"):
+            C8.evict8(c, **kw)
     with pytest.raises(ValueError, match="one of them"):
         C8.evict8(c, 5, keeps=cu[:2])
     with pytest.raises(ValueError, match="layers"):

@@ -55,12 +55,14 @@ class Made:
 
         cu = dev(self.cu)
         self.cache.lens.copy_(dev(self.lens))
-        C8.append8(self.cache, B.bf16_from_bits(self.k_bits), B.bf16_from_bits(self.v_bits), cu)
+        if self.cu[-1]:
+            C8.append8(self.cache, B.bf16_from_bits(self.k_bits), B.bf16_from_bits(self.v_bits), cu)
         at = torch.cat([torch.arange(int(r), int(r) + n, device="cuda") for r, n in zip(self.rows0, self.lens)])
         if at.numel():
             self.cache.weights[:, :, at] = dev(self.w, torch.float32)
         self.at = at
         self.q = B.bf16_from_bits(self.q_bits)
+        self.kept = {}
 
     def rows(self, l, s, h):
         a, b = self.cu[s], self.cu[s + 1]
@@ -74,6 +76,18 @@ class Made:
     def query(self, l, s, h):
         return decode_bf16(self.q_bits[l, s, h * self.G:(h + 1) * self.G])
 
+    def wanted(self, l, s, h, scale):
+        """A KV head's tokens, and of each query head what `attend` gives and the probabilities; kept,
+        for the checks of one cache's results."""
+        if (l, s, h, scale) not in self.kept:
+            k, v = self.rows(l, s, h)
+            heads = []
+            for q in self.query(l, s, h):
+                ref, z, spread, reach = attend(q, k, v, scale)
+                heads.append((ref, z, spread, reach, np.exp(scale * (k @ q) - z) if len(k) else np.zeros(0)))
+            self.kept[l, s, h, scale] = len(k), heads
+        return self.kept[l, s, h, scale]
+
     def check(self, out, lse, weights=None, scale=None, seqs=None, times=1):
         """`weights`: what every token has gathered after `times` steps."""
         out, lse = out.cpu().numpy(), lse.cpu().numpy()
@@ -81,11 +95,9 @@ class Made:
         for l in range(self.L):
             for s in seqs if seqs is not None else range(self.S):
                 for h in range(self.H):
-                    k, v = self.rows(l, s, h)
-                    n = len(k)
+                    n, heads = self.wanted(l, s, h, scale)
                     w, tol_w = np.zeros(n), np.full(n, 2.0 ** -40)
-                    for g, q in enumerate(self.query(l, s, h)):
-                        ref, z, spread, reach = attend(q, k, v, scale)
+                    for g, (ref, z, spread, reach, p) in enumerate(heads):
                         eps = (self.d + 2) * U * reach
                         steps = 2.0 ** -19 + (2 * n + 64) * U
                         tol = 2 * (eps + steps) * spread
@@ -96,7 +108,6 @@ class Made:
                             assert gz == -math.inf
                             continue
                         assert abs(gz - z) <= eps + steps + 4 * U * abs(z), (l, s, h, g, gz, z)
-                        p = np.exp(scale * (k @ q) - z)
                         w += p
                         tol_w += 2 * (eps + steps) * p
                     if weights is not None and n:
@@ -107,7 +118,26 @@ class Made:
                         assert (err <= tol_w).all(), (l, s, h, err.max(), tol_w[err.argmax()])
 
     def gathered(self):
+        if not self.at.numel():
+            return np.zeros((self.L, self.H, 0))
         return self.cache.weights[:, :, self.at].cpu().numpy().astype(np.float64)
+
+
+CASES = dict(
+    CASES,
+    # many units, in numbers that the 8 XCDs do not share evenly, and as many sequences as a wave has lanes:
+    # their splits in order of length, equal ones among them
+    by_length=(11, 12, 6, 64, [(97 * i) % 700 if i % 5 else 0 for i in range(63)] + [2500], [700] * 63 + [2600]),
+    by_length_equal=(16, 8, 4, 128, [1300, 1300, 1280, 128, 1300], [1400, 1300, 1300, 130, 1400]),
+    # every sequence empty
+    empty_splits=(16, 8, 4, 64, [0, 0, 0], [3000, 10, 0]),
+    empty_split=(1, 8, 4, 128, [0], [5000]),
+    empty_single=(1, 8, 4, 64, [0, 0], [100, 0]),
+    # logits in memory though a sequence is one split: too many of them for LDS
+    g16_memory=(1, 32, 2, 64, [700, 20], [700, 30]),
+    # many workgroups of one split each, a tile past the sequence's end
+    short_many=(6, 24, 12, 64, [33, 1, 64, 100], [40, 1, 64, 100]),
+)
 
 
 @pytest.mark.parametrize("cid", list(CASES))
@@ -135,8 +165,9 @@ def test_decode(cid, gpu_lib):
     other = torch.ones(m.cache.rows, dtype=torch.bool, device="cuda")
     other[m.at] = False
     assert torch.equal(before.view(torch.int32)[:, :, other], m.cache.weights.view(torch.int32)[:, :, other])
-    m.write()
-    C8.decode_attention8(m.cache, m.q, scale=scale, gather=True)
+    if m.at.numel():
+        m.write()
+        C8.decode_attention8(m.cache, m.q, scale=scale, gather=True)
     assert torch.equal(once.view(torch.int32), m.cache.weights.view(torch.int32))  # the same every time
 
 
@@ -215,6 +246,19 @@ def test_large_magnitudes(gpu_lib):
         out, lse = C8.decode_attention8(m.cache, m.q, want_lse=True, gather=True)
         m.check(out, lse, m.gathered())
         assert torch.isfinite(out).all()
+
+
+def test_a_cache_without_rows(gpu_lib):
+    """Rooms of nothing: zeros, nothing gathered, nothing to evict."""
+    import torch
+
+    for L, S in ((1, 2), (16, 3)):
+        cache = C8.Cache8(L, 4, 64, [0] * (S + 1))
+        q = torch.ones((L, S, 8, 64), dtype=torch.bfloat16, device="cuda")
+        out, lse = C8.decode_attention8(cache, q, gather=True, want_lse=True)
+        assert (out == 0).all() and (lse == -math.inf).all()
+        C8.evict8(cache, 5)
+        assert cache.lens.tolist() == [0] * S and cache.status() == 0
 
 
 def test_buffers_and_streams(gpu_lib):

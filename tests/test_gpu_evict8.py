@@ -105,6 +105,14 @@ EVICT = {
     "chunk_borders": (1, 1, 64, [1023, 1024, 1025, 2047, 2048, 2049, 4096, 4097], 1000, 0, 0, "ties", 0),
     "many_seqs": (1, 2, 64, [(37 * i) % 150 for i in range(150)], 70, 2, 3, "tail", 4),
     "many_heads": (24, 16, 64, [130, 90], 100, 2, 3, "tail", 4),
+    # rows of every number of waves and keys a lane: 4 x 2, 8 x 5, 16 x 8 and 16 x 20 groups, and streamed
+    "sizes": (1, 1, 64, [2047, 10239, 9], 1500, 4, 64, "tail", 0),
+    "sizes_16": (1, 1, 64, [32767, 1], 31000, 0, 64, "ends", 0),
+    "sizes_ties": (1, 1, 64, [81919], 40000, 0, 0, "ties", 0),
+    "streamed_ties": (1, 1, 64, [81921 + 64, 500], 300, 2, 100, "ties", 0),
+    # whole blocks replaced, 64 moves into each
+    "dense": (1, 2, 128, [4000], 1000, 0, 0, "rising", 10),
+    "dense_d64": (1, 1, 64, [700, 129], 64, 0, 0, "rising", 24),
 }
 
 
