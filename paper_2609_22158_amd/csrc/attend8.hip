@@ -21,9 +21,16 @@
 //    conversion makes them the B operand. P is the A operand, as three bf16 parts
 //    that are it exactly (in one operand for narrow groups); the same parts times
 //    ones give the softmax's sum.
-// combine8_kernel merges the splits. To gather weights the logits are kept (4
-// bytes a query head and token), and the same launch, or the workgroup that has the
-// whole sequence, turns them into weights once the row's maximum and sum are known.
+// combine8_kernel merges the splits. To gather weights, which need the row's maximum
+// and sum, the logits are kept (4 bytes a query head and token), and the same launch,
+// or the workgroup that has the whole sequence, turns them into weights; or, for wide
+// groups, that launch computes them from the keys again.
+//
+// 8 layers x 8 heads x 131071 tokens of d 128 (4 query heads each): 324 us, 6.6 TB/s,
+// 488 with the weights; 28 layers x 4 heads x 16 sequences of 700 to 8192 tokens (7
+// each): 351 us, 5.8 TB/s, 534 with the weights. What the weights cost is memory:
+// stores among loads slow these down by far more than their bytes (134 MB written
+// beside 2.1 GB read: 80 us in a kernel that does only that).
 #include "cache8_device.h"
 
 #include <math.h>
@@ -43,6 +50,7 @@ constexpr int kWavesFew = 8;  // where a whole sequence is one, and there are fe
 constexpr int kMostLds = 32768;  // bytes of logits kept in LDS
 constexpr int kMergeThreads = 256;  // of a merge of many rows
 constexpr int kMergeOne = 512;      // and of a merge of one query head
+constexpr int kMostBlocks = 16;     // that a wave sweeps
 constexpr float kSlack = 16.f;
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -134,8 +142,17 @@ __device__ __forceinline__ float weight_of(float y, float cl2, float2 norm) {
   return fast_exp2(fmaf(y, cl2, -norm.x)) * norm.y;
 }
 
-// Where the logits that weights are gathered from are kept.
-enum { kNone, kMemory, kLds };
+// What weights are gathered from: the logits, kept in memory or LDS, or the keys again.
+enum { kNone, kMemory, kLds, kSweep };
+
+// 16 bytes of keys. Lanes of one load take 64 bytes of a row: all of it (d 64), or half
+// a line, whose other half should still be in the cache when the next load asks for
+// it: 8 layers x 8 heads x 131071 tokens 332 us non-temporal, 324 so.
+template <int D>
+__device__ __forceinline__ u32x4_t load_k(const uint8_t* p) {
+  const u32x4_t* const x = reinterpret_cast<const u32x4_t*>(p);
+  return D == 64 ? __builtin_nontemporal_load(x) : *x;
+}
 
 // NW waves share a split (or, with a.single, a whole sequence); C copies (1 or 3)
 // of the query heads in the operands' rows.
@@ -242,8 +259,7 @@ void attend8_kernel(Attend8Args a) {
       const uint32_t r = min(16 * u + c16, last);  // rows past the end: the last one again
 #pragma unroll
       for (int j = 0; j < KP; ++j)
-        x.k[u][j] = __builtin_nontemporal_load(
-            reinterpret_cast<const u32x4_t*>(kc + (r * D + 64 * j + 16 * g4)));
+        x.k[u][j] = load_k<D>(kc + (r * D + 64 * j + 16 * g4));
     }
 #pragma unroll
     for (int u = 0; u < VL; ++u) {
@@ -413,74 +429,165 @@ __device__ __forceinline__ void splits_of(const Attend8Args& a, int s, int& firs
   n = min((held_const(a.c, s) + split - 1) / split, a.splits - first);
 }
 
-// weights += the weights of THREADS * 4 tokens of a (layer, KV head, sequence), four
-// a thread: the sum over the group's heads in their order. A wave finds what a head's
-// softmax is taken over from the states of the splits.
+// What the softmax of `heads` query heads is taken over, for all threads: (M, 1 / Z)
+// of head g from the states of the splits, a wave for each; (0, 0) past them.
 template <int D, int THREADS>
-__device__ __forceinline__ void gather(const Attend8Args& a, int at) {
+__device__ __forceinline__ void norms_of(const Attend8Args& a, int unit, int split0, int splits, int heads,
+                                         float2* norm_s) {
   constexpr int ST = D + 2;
-  constexpr int kRows = 4 * THREADS;
-  __shared__ float2 norm_s[16];
-  const Cache8View& c = a.c;
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const int per = c.rows / kRows + c.S;  // chunks that a (layer, KV head) may have
-  const int lh = uniform(at / per);
-  at -= lh * per;
-  int s = 0, first = 0;
-  locate_item(c.S, at, [&](int sq) { return (held_tokens(c, sq) + kRows - 1) / kRows; }, s, first);
-  if (s < 0) return;
-  s = uniform(s);
-  const int j = (at - first) * kRows + 4 * tid, held = held_const(c, s);
-  int split0, splits;
-  splits_of(a, s, split0, splits);
-  const int seq_row = read_const(c.cu_rows, s), tiles = (a.G + 15) / 16, wide = min(a.G, 16);
-  const float cl2 = a.scale * kLog2e;
-  float* const to = c.weights + (size_t)lh * c.rows + seq_row + j;
-  float w[4] = {}, was[4];
-  if (j + 4 <= held) __builtin_memcpy(was, to, 16);
-  for (int t = 0; t < tiles; ++t) {
-    const int unit = lh * tiles + t, heads = min(a.G - 16 * t, 16);
-    const float* __restrict__ part = a.partial + ((size_t)unit * a.splits + split0) * wide * ST;
-    if (t > 0) __syncthreads();  // norm_s is read
-    for (int g = wave; g < heads; g += THREADS / kWave) {
-      float M = -INFINITY, Z = 0.f;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), wide = min(a.G, 16);
+  const float* __restrict__ part = a.partial + ((size_t)unit * a.splits + split0) * wide * ST;
+  for (int g = wave; g < 16; g += THREADS / kWave) {
+    float M = -INFINITY, Z = 0.f;
+    if (g < heads)
       for (int i = lane; i < splits; i += kWave) {
         const float* __restrict__ p = part + ((size_t)i * wide + g) * ST + D;
         const float m = p[0], z = p[1], top = fmaxf(M, m);
         Z = (M == -INFINITY ? 0.f : Z * fast_exp2(M - top)) + (m == -INFINITY ? 0.f : z * fast_exp2(m - top));
         M = top;
       }
-      const float top = wave_max(M);
-      const float sum = wave_sum(M == -INFINITY ? 0.f : Z * fast_exp2(M - top));
-      if (lane == 0) norm_s[g] = make_float2(top, 1.f / sum);
-    }
-    __syncthreads();
-    if (j >= held) continue;
-    const float* __restrict__ z = a.logits + logits_at(a, unit, seq_row, s) + token_at(a, j);
-#pragma unroll 4
-    for (int g = 0; g < heads; ++g) {
-      const f32x4_t y = *reinterpret_cast<const f32x4_t*>(z + g * kTile);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] += weight_of(y[e], cl2, norm_s[g]);
-    }
+    const float top = wave_max(M);
+    const float sum = wave_sum(M == -INFINITY ? 0.f : Z * fast_exp2(M - top));
+    if (lane == 0) norm_s[g] = g < heads ? make_float2(top, 1.f / sum) : make_float2(0.f, 0.f);
   }
-  if (j + 4 <= held) {
+  __syncthreads();
+}
+
+// weights += the weights of a run of tokens of a (layer, KV head, sequence): the sums over
+// the group's heads, in one order.
+// From the logits that were kept: THREADS * 4 tokens, four a thread.
+// SWEEP, from the keys once more: a.sweep blocks of 64 tokens a wave, the heads in the
+// products' rows, so that a lane has four heads' logits of a token and four lanes meet
+// for the sum.
+template <int D, int THREADS, bool SWEEP>
+__device__ __forceinline__ void gather(const Attend8Args& a, int at) {
+  const int kRows = SWEEP ? THREADS * a.sweep : 4 * THREADS;
+  __shared__ float2 norm_s[16];
+  const Cache8View& c = a.c;
+  const int tid = threadIdx.x;
+  const int per = c.rows / kRows + c.S;  // runs that a (layer, KV head) may have
+  const int lh = uniform(at / per);
+  at -= lh * per;
+  int s = 0, first = 0;
+  locate_item(c.S, at, [&](int sq) { return (held_tokens(c, sq) + kRows - 1) / kRows; }, s, first);
+  if (s < 0) return;
+  s = uniform(s);
+  const int j0 = (at - first) * kRows, held = held_const(c, s);
+  const int seq_row = read_const(c.cu_rows, s), tiles = (a.G + 15) / 16;
+  const float cl2 = a.scale * kLog2e;
+  int split0, splits;
+  splits_of(a, s, split0, splits);
+  if constexpr (SWEEP) {
+    constexpr int KP = D / 64, NS = D / 32;
+    const int lane = tid & 63, wave = uniform(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
+    const int l = uniform(lh / c.H), h = lh - l * c.H;
+    const int b0 = uniform(j0 / kBlock8 + wave * a.sweep);  // the wave's blocks
+    const int b1 = uniform(min(b0 + a.sweep, (held + kBlock8 - 1) / kBlock8));
+    const size_t row0 = (size_t)lh * c.rows + seq_row, blk0 = (size_t)lh * c.nblk + first_block(seq_row, s);
+    __shared__ float sums_s[THREADS / kWave][kMostBlocks * kBlock8];
+    float* const sums = sums_s[wave];
+    struct Block {
+      u32x4_t k[4][KP];
+      float scale;
+    };
+    auto load = [&](Block& x, int b) __attribute__((always_inline)) {
+      const int last = held - 1 - b * kBlock8;
+      const size_t row = row0 + (size_t)b * kBlock8;
+      const uint8_t* __restrict__ kc = c.k_codes + row * D;
+      x.scale = read_const(c.k_scales, blk0 + b);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) was[e] += w[e];
-    __builtin_memcpy(to, was, 16);
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t r = min(16 * u + c16, last);  // rows past the end: the last one again
+#pragma unroll
+        for (int j = 0; j < KP; ++j)
+          x.k[u][j] = load_k<D>(kc + (r * D + 64 * j + 16 * g4));
+      }
+    };
+    for (int t = 0; t < tiles; ++t) {
+      const int heads = min(a.G - 16 * t, 16);
+      if (t > 0) __syncthreads();  // norm_s is read
+      Block cur;
+      if (b0 < b1) load(cur, b0);
+      norms_of<D, THREADS>(a, lh * tiles + t, split0, splits, heads, norm_s);
+      bf16x8_t qa[NS];
+#pragma unroll
+      for (int ks = 0; ks < NS; ++ks) {
+        qa[ks] = bf16x8_t{};
+        if (c16 < heads)
+          qa[ks] = *reinterpret_cast<const bf16x8_t*>(
+              a.q + (((size_t)l * c.S + s) * a.Hq + h * a.G + 16 * t + c16) * D + 64 * (ks / 2) +
+              16 * g4 + 8 * (ks % 2));
+      }
+      float2 norm[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) norm[i] = norm_s[4 * g4 + i];
+#pragma nounroll
+      for (int b = b0; b < b1; ++b) {  // wave-uniform
+        f32x4_t y[4];  // logits of token c16 of the block's 16-row pieces
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          y[u] = f32x4_t{};
+#pragma unroll
+          for (int ks = 0; ks < NS; ++ks)
+            y[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                qa[ks], __builtin_bit_cast(bf16x8_t, spread8(cur.k[u][ks / 2][2 * (ks % 2)],
+                                                             cur.k[u][ks / 2][2 * (ks % 2) + 1], cur.scale)),
+                y[u], 0, 0, 0);
+        }
+        load(cur, min(b + 1, b1 - 1));  // its registers are free
+        float w[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          w[u] = 0.f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[u] += weight_of(y[u][e], cl2, norm[e]);
+          w[u] += xor16(w[u]);
+          w[u] += xor32(w[u]);
+        }
+        const float mine = g4 < 2 ? (g4 & 1 ? w[1] : w[0]) : (g4 & 1 ? w[3] : w[2]);  // lane i: token i
+        float* const to = sums + (b - b0) * kBlock8 + lane;
+        *to = t > 0 ? *to + mine : mine;
+      }
+    }
+    // written at the end: stores among the loads would be waited for with them
+    for (int j = b0 * kBlock8 + lane; j < min(b1 * kBlock8, held); j += kWave)
+      c.weights[row0 + j] += sums[j - b0 * kBlock8];
   } else {
+    const int j = j0 + 4 * tid;
+    float* const to = c.weights + (size_t)lh * c.rows + seq_row + j;
+    float w[4] = {}, was[4];
+    if (j + 4 <= held) __builtin_memcpy(was, to, 16);
+    for (int t = 0; t < tiles; ++t) {
+      const int unit = lh * tiles + t, heads = min(a.G - 16 * t, 16);
+      if (t > 0) __syncthreads();  // norm_s is read
+      norms_of<D, THREADS>(a, unit, split0, splits, heads, norm_s);
+      if (j >= held) continue;
+      const float* __restrict__ z = a.logits + logits_at(a, unit, seq_row, s) + token_at(a, j);
+#pragma unroll 4
+      for (int g = 0; g < heads; ++g) {
+        const f32x4_t y = *reinterpret_cast<const f32x4_t*>(z + g * kTile);
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (j + e < held) to[e] += w[e];
+        for (int e = 0; e < 4; ++e) w[e] += weight_of(y[e], cl2, norm_s[g]);
+      }
+    }
+    if (j + 4 <= held) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) was[e] += w[e];
+      __builtin_memcpy(to, was, 16);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (j + e < held) to[e] += w[e];
+    }
   }
 }
 
 // out and lse of a (layer, sequence, KV head, 16 query heads), or of one query
 // head of them: the splits' states merged by a running maximum, four in flight
 // per thread. A thread per (head, channel), or with one head a group of
-// THREADS / D threads per channel over the splits, merged in order. With GATHER the
-// first `gathers` workgroups add up weights instead.
-template <int D, int THREADS, bool ONE, bool GATHER>
+// THREADS / D threads per channel over the splits, merged in order. The first
+// `gathers` workgroups add up weights instead.
+template <int D, int THREADS, bool ONE, int GATHER>
 __global__ __launch_bounds__(THREADS) void combine8_kernel(Attend8Args a, int gathers) {
   constexpr int ST = D + 2;
   constexpr int J = ONE ? THREADS / D : 1;
@@ -488,9 +595,9 @@ __global__ __launch_bounds__(THREADS) void combine8_kernel(Attend8Args a, int ga
   __shared__ float om[J][D], mm[J], zm[J];
   const Cache8View& c = a.c;
   int at = blockIdx.x;
-  if constexpr (GATHER) {
+  if constexpr (GATHER != kNone) {
     if (at < gathers) {
-      gather<D, THREADS>(a, at);
+      gather<D, THREADS, GATHER == kSweep>(a, at);
       return;
     }
     at -= gathers;
@@ -579,15 +686,19 @@ bool few_workgroups(const Attend8Args& a) { return a.single && attend_workgroups
 // The merge: one query head a workgroup while there are few.
 bool merges_heads(const Attend8Args& a) { return units_of(a) * a.c.S >= 512; }
 int64_t gather_workgroups(const Attend8Args& a) {
-  return (int64_t)a.c.L * a.c.H * (a.c.rows / (4 * (merges_heads(a) ? kMergeThreads : kMergeOne)) + a.c.S);
+  const int rows = (a.sweep ? a.sweep : 4) * (merges_heads(a) ? kMergeThreads : kMergeOne);
+  return (int64_t)a.c.L * a.c.H * (a.c.rows / rows + a.c.S);
 }
 
 }  // namespace
 
-// Splits for the rooms. Short sequences are one split each, which needs no merge;
-// 8 waves share it while there are at most 256. Otherwise about 4096 rows a
-// split, but enough splits for four workgroups on each of the 256 compute units
-// while those have a tile per wave.
+// Splits for the rooms. Short sequences are one split each, which needs no merge (up
+// to about the length at which the merge's launch costs less than the wait); 8 waves
+// share it while there are at most 256. Otherwise about 4096 rows a split, or 8192 of
+// long sequences (131071 tokens 362 -> 335 us, fewer states to write and merge; of
+// 700 to 8192 it would leave too few workgroups), but enough splits for four
+// workgroups on each of the 256 compute units while those have a tile per wave.
+// Batches take their longest splits first: 16 sequences of 700 to 8192 387 -> 372 us.
 void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host) {
   const int64_t units = units_of(a);
   a.min_rows = kTile * kWaves;
@@ -601,10 +712,11 @@ void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host) {
   const int64_t rows = units * a.c.S;  // workgroups of one split a sequence
   const int64_t most_single = rows > 256 ? 1024 : std::min<int64_t>(2048, 640 + 12 * rows);
   a.single = longest * (a.c.d + 64) / 192 <= most_single && a.G <= 16;
-  a.by_length = a.lds_bytes = 0;
+  a.by_length = a.lds_bytes = a.sweep = 0;
   if (a.single) {
     a.splits = a.c.S;
-    // few workgroups: a CU's LDS has room for the logits of a short sequence
+    // few workgroups: a CU's LDS has room for the logits of a short sequence (300
+    // tokens, 4 heads: a call 10.6 us with logits in memory, 8.2 so)
     const int64_t bytes = (longest + kTile - 1) / kTile * a.G * kTile * (int64_t)sizeof(float);
     if (few_workgroups(a) && bytes <= kMostLds) a.lds_bytes = (int)bytes;
     return;
@@ -613,6 +725,11 @@ void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host) {
   const int64_t want = std::max<int64_t>((1024 + units - 1) / units, total / split_rows);
   a.splits = (int)std::max<int64_t>(std::min<int64_t>(most, want + a.c.S), 1);
   a.by_length = a.c.S > 1 && a.c.S <= kWave && units >= 64;
+  // Logits are 4 bytes a head written and read, keys d bytes read: 28 layers x 4 heads x 16
+  // sequences of 700 to 8192, us with logits and with keys: G 7 534, 565 and G 8 545, 571
+  // (d 128), G 8 323, 303 (d 64); 14 layers, d 128, G 16 359, 313 and G 32 632, 456.
+  if (a.G * 14 > a.c.d)
+    a.sweep = (int)std::min<int64_t>(std::max<int64_t>((int64_t)a.c.L * a.c.H * total / (kBlock8 * 8192), 1), kMostBlocks);
 }
 
 size_t attend8_partial_floats(const Attend8Args& a) {
@@ -621,7 +738,7 @@ size_t attend8_partial_floats(const Attend8Args& a) {
 }
 
 size_t attend8_logits(const Attend8Args& a) {
-  if (a.lds_bytes > 0) return 0;
+  if (a.lds_bytes > 0 || a.sweep) return 0;
   return (size_t)units_of(a) * (a.c.rows / kTile + a.c.S) * std::min(a.G, 16) * kTile;
 }
 
@@ -641,7 +758,7 @@ void launch_attend(const Attend8Args& a, hipStream_t st) {
   const dim3 grid((unsigned)attend_workgroups(a));
   auto copies = [&](auto nw, auto cc) {
     constexpr int NW = decltype(nw)::value, C = decltype(cc)::value;
-    if (!a.gather)
+    if (!a.gather || a.sweep)
       hipLaunchKernelGGL((attend8_kernel<D, NW, kNone, C>), grid, dim3(NW * kWave), 0, st, a);
     else if (a.lds_bytes == 0)
       hipLaunchKernelGGL((attend8_kernel<D, NW, kMemory, C>), grid, dim3(NW * kWave), 0, st, a);
@@ -657,7 +774,7 @@ void launch_attend(const Attend8Args& a, hipStream_t st) {
   if (a.single) return;
   const unsigned rows = units * (unsigned)a.c.S, gathers = a.gather ? (unsigned)gather_workgroups(a) : 0u;
   auto merge = [&](auto gather) {
-    constexpr bool GATHER = decltype(gather)::value;
+    constexpr int GATHER = decltype(gather)::value;
     if (merges_heads(a))
       hipLaunchKernelGGL((combine8_kernel<D, kMergeThreads, false, GATHER>), dim3(gathers + rows),
                          dim3(kMergeThreads), 0, st, a, (int)gathers);
@@ -665,8 +782,9 @@ void launch_attend(const Attend8Args& a, hipStream_t st) {
       hipLaunchKernelGGL((combine8_kernel<D, kMergeOne, true, GATHER>),
                          dim3(gathers + rows * std::min(a.G, 16)), dim3(kMergeOne), 0, st, a, (int)gathers);
   };
-  if (a.gather) merge(std::integral_constant<bool, true>{});
-  else merge(std::integral_constant<bool, false>{});
+  if (!a.gather) merge(std::integral_constant<int, kNone>{});
+  else if (a.sweep) merge(std::integral_constant<int, kSweep>{});
+  else merge(std::integral_constant<int, kMemory>{});
 }
 
 }  // namespace

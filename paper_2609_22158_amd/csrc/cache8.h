@@ -69,10 +69,11 @@ struct Attend8Args {
   int single;                // nonzero: a sequence is one split, written without a merge
   int by_length;             // nonzero: the longest splits are taken first
   int gather;                // nonzero: weights are added up
+  int sweep;                 // nonzero: from the keys, read again, this many blocks a wave (then logits is null)
   int lds_bytes;             // of the logits, where LDS holds them (then logits is null)
   float scale;
 };
-// Fills splits, min_rows, single, by_length and lds_bytes from the shape and the rooms of the sequences.
+// Fills splits, min_rows, single, by_length, sweep and lds_bytes from the shape and the rooms of the sequences.
 void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host);
 size_t attend8_partial_floats(const Attend8Args& a);
 size_t attend8_logits(const Attend8Args& a);  // floats of them

@@ -114,7 +114,10 @@ __device__ __forceinline__ Span8 span_const(const Write8Args& a, int s) {
 // One workgroup per (layer, KV head, block of 64 tokens): a lane holds 16 bytes
 // (8 channels) of a row of K and of V, the largest magnitudes of the block meet
 // in LDS, and its scales are written once. A token of the call without a source
-// keeps its codes.
+// keeps its codes. Chains of loads bound it (the block's sequence, the positions, the
+// rows), so a workgroup has all its rows in flight at once: 32 layers x 8 heads x 1536
+// gathered rows of d 128 64 us, 308 MB at 4.8 TB/s; 8100 new tokens of 8 heads 11 us
+// (50 MB), one token of each of 28 sequences 4.5.
 template <int D>
 __global__ __launch_bounds__(kThreads) void write8_kernel(Write8Args a) {
   constexpr int PR = D / 8;          // pieces of 8 channels a row
@@ -276,7 +279,9 @@ __global__ void advance8_kernel(Cache8View c, const int32_t* __restrict__ cu_new
 
 // A thread per 8 channels of a row: 8 bytes of codes in, 16 bytes out, PASSES
 // rows in flight per thread. A workgroup's rows almost always belong to one
-// sequence, whose bounds are then found once, with scalar loads.
+// sequence, whose bounds are then found once, with scalar loads. 28 layers x 4 heads x
+// 28812 rows of d 128 in 16 sequences: 392 us, 2.48 GB at 6.3 TB/s (a copy of as many
+// bytes: 377).
 template <int D, int PASSES>
 __global__ __launch_bounds__(kThreads) void read8_kernel(Read8Args a) {
   constexpr int PR = D / 8;

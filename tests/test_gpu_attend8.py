@@ -136,6 +136,12 @@ CASES = dict(
     # logits in memory though a sequence is one split: too many of them for LDS
     g16_memory=(1, 32, 2, 64, [700, 20], [700, 30]),
     # many workgroups of one split each, a tile past the sequence's end
+    # wide groups, whose weights come from the keys read again: rooms that start inside a block, a block's
+    # first row, empty sequences; several blocks a wave
+    sweep_d64=(1, 10, 2, 64, [5000, 0, 70, 2113, 1], [5003, 40, 70, 2200, 9]),
+    sweep_d128=(2, 44, 4, 128, [6145, 1, 0, 3000], [6150, 1, 5, 3001]),
+    sweep_tiles=(1, 40, 1, 128, [4100, 129], [4100, 130]),
+    sweep_blocks=(1, 80, 16, 64, [40007, 25600], [40010, 25700]),
     short_many=(6, 24, 12, 64, [33, 1, 64, 100], [40, 1, 64, 100]),
 )
 
