@@ -239,6 +239,77 @@ def test_logits_that_overflow(rooms, gpu_lib):
             assert (w - torch.from_numpy(m.w[0, 0]).double() - 2 / 199).abs()[torch.arange(200) != 50].max() < 1e-6
 
 
+def test_wide_groups_not_a_number_and_overflow(gpu_lib):
+    """As above where the weights come from the keys read again, 11 heads beside 5 empty rows of the products."""
+    import torch
+
+    m = Made("wide nan", 1, 22, 2, 64, [400, 300, 200], [4000, 3000, 2000])
+    m.q_bits[0, 2, 15, 7] = 0x7FC0            # sequence 2, KV head 1
+    m.k_bits[0, 350, 1, 3] = 0x7F80           # an infinite key of sequence 0, KV head 1
+    m.v_bits[0, 400 + 299, 0, 60] = 0xFFC0    # no weight depends on a value
+    m.write()
+    out, lse = C8.decode_attention8(m.cache, m.q, want_lse=True, gather=True)
+    w = np.isnan(m.gathered())[0]
+    assert w[1, :400].all() and w[1, 700:].all() and not w[1, 400:700].any() and not w[0].any()
+    m.write()
+    m.cache.lens.copy_(dev([350, 299, 200]))
+    C8.decode_attention8(m.cache, m.q, gather=True)
+    w = m.gathered()[0]
+    assert np.isfinite(w[:, :700]).all() and np.array_equal(w[:, 350:400], m.w[0, :, 350:400])
+    for sign, where, finite in ((-1, slice(0, 200), False), (1, slice(50, 51), False), (-1, slice(50, 51), True)):
+        m = Made("wide over", 1, 11, 1, 64, [200], [3000])
+        m.q_bits[:] = f32_to_bf16_bits(np.full(m.q_bits.shape, 1.0e20, np.float32))
+        k = np.zeros((1, 200, 1, 64), np.float32)
+        k[0, where] = sign * 1.0e20
+        m.k_bits = f32_to_bf16_bits(k)
+        m.write()
+        C8.decode_attention8(m.cache, m.q, gather=True)
+        w = torch.from_numpy(m.gathered()[0, 0])
+        if not finite:
+            assert torch.isnan(w).all()
+        else:
+            assert w[50] == m.w[0, 0, 50]
+            # 11 weights of 1/199 within 2^-19 each, then 12 additions of numbers up to 1.06
+            err = (w - torch.from_numpy(m.w[0, 0]).double() - 11 / 199).abs()
+            assert err[torch.arange(200) != 50].max() < 11 / 199 * 2.0 ** -18 + 12 * 1.06 * U
+
+
+@pytest.mark.parametrize("Hq", [8, 22], ids=["logits", "keys"])
+def test_replays_as_the_cache_grows(Hq, gpu_lib):
+    """A gathering step over split sequences captured once and replayed while the cache grows past the
+    borders of tiles, blocks and splits, with eager work between the replays: the eager steps' bits."""
+    import torch
+
+    rng = np.random.default_rng(Hq)
+    caches = [C8.Cache8(2, 2, 64, [0, 3000, 6001]) for _ in range(2)]
+    first = B.bf16_from_bits(f32_to_bf16_bits(rng.standard_normal((2, 2700, 2, 64)).astype(np.float32)))
+    for c in caches:
+        C8.advance8(c, dev([0, 2000, 2700]))
+        C8.append8(c, first, first, dev([0, 2000, 2700]))
+    x, q = first[:, :61].clone(), first[:, :2].repeat(1, 1, Hq // 2, 1).contiguous()
+    cu, side, outs = dev([0, 40, 61]), torch.cuda.Stream(), [None, None]
+
+    def step(i):
+        C8.advance8(caches[i], cu)
+        C8.append8(caches[i], x, x, cu)
+        outs[i] = C8.decode_attention8(caches[i], q, gather=True)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(1)
+    for i in range(20):
+        x.copy_(first[:, 100 * i:100 * i + 61])
+        q.copy_(first[:, 7 * i:7 * i + 2].repeat(1, 1, Hq // 2, 1))
+        graph.replay()
+        step(0)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[1]), i
+        for name in ("lens", "weights", "k_codes", "v_codes", "k_scales"):
+            assert torch.equal(getattr(caches[0], name), getattr(caches[1], name)), (i, name)
+    assert caches[0].lens.tolist() == [2800, 1120] and caches[0].status() == 0
+
+
 def test_large_magnitudes(gpu_lib):
     """Keys near the greatest scale against tiny queries, and values at both ends of the range."""
     import torch
