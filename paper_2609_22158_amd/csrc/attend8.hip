@@ -27,8 +27,8 @@
 // groups, that launch computes them from the keys again.
 //
 // 8 layers x 8 heads x 131071 tokens of d 128 (4 query heads each): 324 us, 6.6 TB/s,
-// 488 with the weights; 28 layers x 4 heads x 16 sequences of 700 to 8192 tokens (7
-// each): 351 us, 5.8 TB/s, 534 with the weights. What the weights cost is memory:
+// 486 with the weights; 28 layers x 4 heads x 16 sequences of 700 to 8192 tokens (7
+// each): 351 us, 5.8 TB/s, 523 with the weights. What the weights cost is memory:
 // stores among loads slow these down by far more than their bytes (134 MB written
 // beside 2.1 GB read: 80 us in a kernel that does only that).
 #include "cache8_device.h"
@@ -51,6 +51,7 @@ constexpr int kMostLds = 32768;  // bytes of logits kept in LDS
 constexpr int kMergeThreads = 256;  // of a merge of many rows
 constexpr int kMergeOne = 512;      // and of a merge of one query head
 constexpr int kMostBlocks = 16;     // that a wave sweeps
+constexpr int kMostLogits = 9;      // heads of a group whose logits are kept for the merge
 constexpr float kSlack = 16.f;
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -455,7 +456,8 @@ __device__ __forceinline__ void norms_of(const Attend8Args& a, int unit, int spl
 
 // weights += the weights of a run of tokens of a (layer, KV head, sequence): the sums over
 // the group's heads, in one order.
-// From the logits that were kept: THREADS * 4 tokens, four a thread.
+// From the logits that were kept, of at most kMostLogits heads: THREADS * 4 tokens, four a
+// thread.
 // SWEEP, from the keys once more: a.sweep blocks of 64 tokens a wave, the heads in the
 // products' rows, so that a lane has four heads' logits of a token and four lanes meet
 // for the sum.
@@ -473,12 +475,13 @@ __device__ __forceinline__ void gather(const Attend8Args& a, int at) {
   if (s < 0) return;
   s = uniform(s);
   const int j0 = (at - first) * kRows, held = held_const(c, s);
-  const int seq_row = read_const(c.cu_rows, s), tiles = (a.G + 15) / 16;
+  const int seq_row = read_const(c.cu_rows, s);
   const float cl2 = a.scale * kLog2e;
-  int split0, splits;
-  splits_of(a, s, split0, splits);
   if constexpr (SWEEP) {
+    int split0, splits;
+    splits_of(a, s, split0, splits);
     constexpr int KP = D / 64, NS = D / 32;
+    const int tiles = (a.G + 15) / 16;
     const int lane = tid & 63, wave = uniform(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
     const int l = uniform(lh / c.H), h = lh - l * c.H;
     const int b0 = uniform(j0 / kBlock8 + wave * a.sweep);  // the wave's blocks
@@ -556,20 +559,24 @@ __device__ __forceinline__ void gather(const Attend8Args& a, int at) {
     const int j = j0 + 4 * tid;
     float* const to = c.weights + (size_t)lh * c.rows + seq_row + j;
     float w[4] = {}, was[4];
-    if (j + 4 <= held) __builtin_memcpy(was, to, 16);
-    for (int t = 0; t < tiles; ++t) {
-      const int unit = lh * tiles + t, heads = min(a.G - 16 * t, 16);
-      if (t > 0) __syncthreads();  // norm_s is read
-      norms_of<D, THREADS>(a, unit, split0, splits, heads, norm_s);
-      if (j >= held) continue;
-      const float* __restrict__ z = a.logits + logits_at(a, unit, seq_row, s) + token_at(a, j);
-#pragma unroll 4
-      for (int g = 0; g < heads; ++g) {
-        const f32x4_t y = *reinterpret_cast<const f32x4_t*>(z + g * kTile);
+    f32x4_t y[kMostLogits];  // in flight while the norms are found
+    if (j < held) {
+      const float* __restrict__ z = a.logits + logits_at(a, lh, seq_row, s) + token_at(a, j);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] += weight_of(y[e], cl2, norm_s[g]);
-      }
+      for (int g = 0; g < kMostLogits; ++g)
+        if (g < a.G) y[g] = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(z + g * kTile));
+      if (j + 4 <= held) __builtin_memcpy(was, to, 16);
     }
+    int split0, splits;
+    splits_of(a, s, split0, splits);
+    norms_of<D, THREADS>(a, lh, split0, splits, a.G, norm_s);
+    if (j >= held) return;
+#pragma unroll
+    for (int g = 0; g < kMostLogits; ++g)
+      if (g < a.G) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] += weight_of(y[g][e], cl2, norm_s[g]);
+      }
     if (j + 4 <= held) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) was[e] += w[e];
@@ -726,9 +733,9 @@ void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host) {
   a.splits = (int)std::max<int64_t>(std::min<int64_t>(most, want + a.c.S), 1);
   a.by_length = a.c.S > 1 && a.c.S <= kWave && units >= 64;
   // Logits are 4 bytes a head written and read, keys d bytes read: 28 layers x 4 heads x 16
-  // sequences of 700 to 8192, us with logits and with keys: G 7 534, 565 and G 8 545, 571
+  // sequences of 700 to 8192, us with logits and with keys: G 7 523, 565 and G 8 536, 571
   // (d 128), G 8 323, 303 (d 64); 14 layers, d 128, G 16 359, 313 and G 32 632, 456.
-  if (a.G * 14 > a.c.d)
+  if (a.G * 14 > a.c.d || a.G > kMostLogits)
     a.sweep = (int)std::min<int64_t>(std::max<int64_t>((int64_t)a.c.L * a.c.H * total / (kBlock8 * 8192), 1), kMostBlocks);
 }
 
