@@ -36,10 +36,13 @@
  *   code  = x / 2^e rounded to the nearest e4m3 number, ties to even, at most
  *         448; a NaN or an infinity is held as NaN.
  *   value = element * 2^e, exact in bf16.
- * An element is off by at most 2^-4 of it, or by 2^-9 * 2^e if that is more,
- * however often its block grew (powers of two move e4m3 numbers without a
- * rounding above 2^-6). Quantising rows that were read back, block by block,
- * gives the same values.
+ * An element of magnitude up to 464 * 2^119 is off by at most 2^-4 of it, or by
+ * 2^-9 * 2^E if that is more, where E is the greatest exponent that a block had
+ * while it held the element: its block's e, however often that grew (powers of
+ * two move e4m3 numbers without a rounding above 2^-6), and, of a row that
+ * eviction moved, those of the blocks that it was in before too. Finite elements
+ * of greater magnitude are held as 448 * 2^119, the greatest bf16 value 12.2% low.
+ * Quantising rows that were read back, block by block, gives the same values.
  *
  * Layouts (L layers, H KV heads, d head dim, R = cu_rows[S] rows, S sequences):
  *   k_codes, v_codes    uint8 [L][H][R][d]  16-byte aligned
