@@ -170,11 +170,11 @@ size_t stepkv_cache8_decode_workspace_bytes(const stepkv_cache8* c, int32_t num_
  * result is NaN, the log-sum-exp -inf and the tokens' weights NaN. A NaN in an
  * attended key, value or query makes its results NaN (in a key or query also the
  * weights of the KV head's tokens), and so does a logit that overflows to +inf.
- * fp32 sums of exact products, the probabilities in fp32, up to 2^16 before they
- * are divided by their sum: sums over values past about 2^111 may overflow.
- * Results are the same from call to call. What other sequences hold does not
- * enter them; how many tokens they hold may move the borders of the splits, and
- * so change the last bits.
+ * fp32 sums of exact products; the probabilities, in fp32 and up to 2^16, are
+ * divided by their sum after the n tokens' products with the values were added up:
+ * of values past 2^111 / n these may overflow. Results are the same from call to
+ * call. What other sequences hold does not enter them; how many tokens they hold
+ * may move the borders of the splits, and so change the last bits.
  * Errors: EINVAL (also a scale whose product with log2(e) overflows, gather on a
  * cache without weights), EUNSUPPORTED (d, rows), EWORKSPACE (below
  * stepkv_cache8_decode_workspace_bytes, or not 256-byte aligned), EHIP. */
