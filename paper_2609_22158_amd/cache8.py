@@ -91,7 +91,9 @@ class Cache8:
     The buffers are allocated (zeroed) unless given. ``weights`` and ``positions`` are what
     gathering and evicting need: ``weights=False`` keeps neither, for caches that only grow
     between boundaries. ``lens`` (int32 [S]) counts each sequence's tokens, ``seen`` those that
-    came so far; given ``lens`` that are not 0 need the ``seen`` that go with them."""
+    came so far. Given tokens (``lens`` that are not 0) without ``seen`` are all that came, and
+    without ``positions`` they are the last that came, in order: seen[s] - lens[s] + j for token j.
+    Where tokens were pruned or evicted before, both have to be given."""
 
     def __init__(self, num_layers: int, num_kv_heads: int, head_dim: int, cu_rows, *, k_codes=None,
                  v_codes=None, k_scales=None, v_scales=None, weights=True, positions=None,
@@ -127,6 +129,15 @@ class Cache8:
             self.positions = buffer(positions, torch.int32, (L, H, R), "positions")
         self.lens = buffer(lens, torch.int32, (S,), "lens")
         self.seen = buffer(seen, torch.int32, (S,), "seen")
+        if lens is not None:
+            if seen is None:
+                self.seen.copy_(self.lens)
+            if self.positions is not None and positions is None:
+                cu = self.cu_rows_dev.long()
+                s = torch.repeat_interleave(torch.arange(S, device=dev), cu[1:] - cu[:-1], output_size=R)
+                j = torch.arange(R, device=dev) - cu[s]
+                held = self.lens[s]
+                self.positions.copy_(torch.where(j < held, self.seen[s] - held + j, 0))
         self.status_dev = torch.zeros(1, dtype=torch.int32, device=dev) if status else None
         self.whole = True  # not some layers of a cache
         load()
