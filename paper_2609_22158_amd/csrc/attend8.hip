@@ -26,9 +26,10 @@
 // or the workgroup that has the whole sequence, turns them into weights; or, for wide
 // groups, that launch computes them from the keys again.
 //
-// 8 layers x 8 heads x 131071 tokens of d 128 (4 query heads each): 324 us, 6.6 TB/s,
-// 486 with the weights; 28 layers x 4 heads x 16 sequences of 700 to 8192 tokens (7
-// each): 351 us, 5.8 TB/s, 523 with the weights. What the weights cost is memory:
+// 8 layers x 8 heads x 131071 tokens of d 128 (4 query heads each): 327 to 335 us, 6.4 to
+// 6.6 TB/s, 489 with the weights; 28 layers x 4 heads x 16 sequences of 700 to 8192 tokens
+// (7 each): 350 us, 5.8 TB/s, 522 with the weights. One layer of these a call, the layers
+// in turn: 56 us (74 with the weights) and 30 (35). What the weights cost is memory:
 // stores among loads slow these down by far more than their bytes (134 MB written
 // beside 2.1 GB read: 80 us in a kernel that does only that).
 #include "cache8_device.h"
@@ -148,7 +149,8 @@ enum { kNone, kMemory, kLds, kSweep };
 
 // 16 bytes of keys. Lanes of one load take 64 bytes of a row: all of it (d 64), or half
 // a line, whose other half should still be in the cache when the next load asks for
-// it: 8 layers x 8 heads x 131071 tokens 332 us non-temporal, 324 so.
+// it: 8 layers x 8 heads x 131071 tokens 346 us non-temporal, 334 so (timed in turn, as
+// the pairs at plan_attend8).
 template <int D>
 __device__ __forceinline__ u32x4_t load_k(const uint8_t* p) {
   const u32x4_t* const x = reinterpret_cast<const u32x4_t*>(p);
@@ -702,10 +704,11 @@ int64_t gather_workgroups(const Attend8Args& a) {
 // Splits for the rooms. Short sequences are one split each, which needs no merge (up
 // to about the length at which the merge's launch costs less than the wait); 8 waves
 // share it while there are at most 256. Otherwise about 4096 rows a split, or 8192 of
-// long sequences (131071 tokens 362 -> 335 us, fewer states to write and merge; of
-// 700 to 8192 it would leave too few workgroups), but enough splits for four
-// workgroups on each of the 256 compute units while those have a tile per wave.
-// Batches take their longest splits first: 16 sequences of 700 to 8192 387 -> 372 us.
+// long sequences (131071 tokens 339 against 334 us, 504 against 489 with weights: fewer
+// states to write and merge; of 700 to 8192 it would leave too few workgroups), but
+// enough splits for four workgroups on each of the 256 compute units while those have
+// a tile per wave. Batches take their longest splits first: 16 sequences of 700 to 8192
+// 366 against 350 us.
 void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host) {
   const int64_t units = units_of(a);
   a.min_rows = kTile * kWaves;
@@ -732,9 +735,16 @@ void plan_attend8(Attend8Args& a, const int32_t* cu_rows_host) {
   const int64_t want = std::max<int64_t>((1024 + units - 1) / units, total / split_rows);
   a.splits = (int)std::max<int64_t>(std::min<int64_t>(most, want + a.c.S), 1);
   a.by_length = a.c.S > 1 && a.c.S <= kWave && units >= 64;
-  // Logits are 4 bytes a head written and read, keys d bytes read: 28 layers x 4 heads x 16
-  // sequences of 700 to 8192, us with logits and with keys: G 7 523, 565 and G 8 536, 571
-  // (d 128), G 8 323, 303 (d 64); 14 layers, d 128, G 16 359, 313 and G 32 632, 456.
+  // Logits are 4 bytes a head written and read, keys d bytes read. us with logits and with
+  // keys, of 28 layers x 4 heads x 16 sequences of 700 to 8192 and of 8 layers x 8 heads x
+  // 131071 tokens:
+  //   d 128  G 8 538, 570 and 549, 572   G 9 551, 576 and 562, 571   G 10 563, 580 and 572, 577
+  //          G 12 585, 583 and 593, 579
+  //   d 64   G 4 290, 312 and 302, 321   G 5 289, 303 and 312, 317   G 7 309, 306 and 333, 318
+  //          G 8 322, 308 and 344, 319
+  // so G 5 at d 64 is up to 5% faster with logits. One layer of them a call is faster with
+  // logits up to G 10: d 128, G 10 37, 48 and 87, 97; d 64, G 8 25, 30 and 53, 57; G 12 at d 64
+  // 30, 32 and 60, 60. (kMostLogits is the widest group that this leaves to the logits.)
   if (a.G * 14 > a.c.d || a.G > kMostLogits)
     a.sweep = (int)std::min<int64_t>(std::max<int64_t>((int64_t)a.c.L * a.c.H * total / (kBlock8 * 8192), 1), kMostBlocks);
 }

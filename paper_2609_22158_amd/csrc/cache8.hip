@@ -115,8 +115,8 @@ __device__ __forceinline__ Span8 span_const(const Write8Args& a, int s) {
 // (8 channels) of a row of K and of V, the largest magnitudes of the block meet
 // in LDS, and its scales are written once. A token of the call without a source
 // keeps its codes. Chains of loads bound it (the block's sequence, the positions, the
-// rows), so a workgroup has all its rows in flight at once: 32 layers x 8 heads x 1536
-// gathered rows of d 128 64 us, 308 MB at 4.8 TB/s; 8100 new tokens of 8 heads 11 us
+// rows), so a workgroup has all its rows in flight at once; blocks go to the XCDs in
+// turn. 32 layers x 8 heads x 1536 gathered rows of d 128 66 us, 308 MB at 4.7 TB/s; 8100 new tokens of 8 heads 11 us
 // (50 MB), one token of each of 28 sequences 4.5.
 template <int D>
 __global__ __launch_bounds__(kThreads) void write8_kernel(Write8Args a) {
